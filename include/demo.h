@@ -347,6 +347,111 @@ demo_status demo_set_path(demo_ctx *ctx, int32_t path);
 typedef enum demo_momentum_domain { DEMO_MOMENTUM_SPATIAL = 0, DEMO_MOMENTUM_DCT = 1 } demo_momentum_domain;
 demo_status demo_set_momentum_domain(demo_ctx *ctx, int32_t domain);
 
+/*
+ * Orthogonalised updates (the Muon optimizer's rule) -- beside the sign of Algorithm 1, another transform of a momentum matrix into an
+ * update: the matrix with its singular values moved towards one by Newton-Schulz iterations,
+ *     X = U / (||U||_F + eps);   steps times:  A = X X^T,  X <- a X + (b A + c A^2) X;   O(U) = X
+ * (for a matrix with more rows than columns of its transpose).  A demo_muon_ctx belongs to a list of matrices, of any sizes from 1 x 1,
+ * and owns the workspace of the iterations: a few matrices at a time, as many as fill the device.
+ *
+ * Accuracy: products of fp16 operands accumulated in fp32; the linear term keeps 22 bits and the diagonal of A stays fp32.  Against
+ * 64 bits O has a relative error (Frobenius norm) of about 1e-3, 1e-5 where the smaller side is at most 256, also where U has low rank.
+ * Coefficients under which singular values grow beyond about 3 in the iterations leave the range of fp16: unspecified values.  NaN or Inf in a
+ * matrix make its own result unspecified and no other's; a matrix of zeros gives zeros.  Results do not depend on the order of
+ * execution: the same call on the same data gives the same bits.
+ *
+ * Device buffers are contiguous, 16-byte aligned and, unless stated, not aliased.  Calls on one context, captured graphs among them, are
+ * issued in stream order as for demo_ctx: they share its workspace.  Pointer arrays are copied to device tables, of each entry point its
+ * own, when they differ from that entry point's last call; a call that would have to copy them on a stream that is being captured
+ * returns INVALID_ARG with nothing enqueued (call it once before).  After demo_muon_set_lr a captured graph keeps the rate it was
+ * captured with.
+ */
+typedef struct demo_muon_ctx demo_muon_ctx; /* opaque, library-owned */
+
+/* The factor s of an update: none; sqrt(max(1, rows / cols)); 0.2 sqrt(max(rows, cols)), which gives the update the size of an AdamW
+ * update (root mean square 0.2), so that the learning rate and the weight decay of one serve the other. */
+typedef enum { DEMO_SCALE_NONE = 0, DEMO_SCALE_ASPECT = 1, DEMO_SCALE_RMS = 2 } demo_update_scale;
+
+typedef struct {
+    float momentum;        /* mu: m <- mu m + g                                                  */
+    int32_t nesterov;      /* 1: U = g + mu m (with the new m); 0: U = m                         */
+    int32_t steps;         /* iterations, 1 .. DEMO_MUON_MAX_STEPS                               */
+    float coefficients[3]; /* a, b, c                                                            */
+    float eps;             /* >= 0                                                               */
+    float lr;
+    float weight_decay;
+    int32_t scale;         /* demo_update_scale                                                  */
+    int32_t grad_dtype;    /* demo_dtype of demo_muon_step's gradients (momentum, params: fp32)  */
+} demo_muon_config;
+#define DEMO_MUON_MAX_STEPS 64
+#define DEMO_MUON_MAX_EXTENT (1 << 20)
+
+/* tensors: descriptors with ndim 2.  Errors: INVALID_ARG (nulls, n_tensors < 1, values not finite, steps, eps, scale), SHAPE (ndim,
+ * extents outside 1 .. DEMO_MUON_MAX_EXTENT), UNSUPPORTED (dtype, more than 2^20 tensors or 2^31 tiles, no tensor-map encoder), ALLOC, CUDA. */
+demo_status demo_muon_init(demo_muon_ctx **out, const demo_muon_config *cfg, const demo_tensor_desc *tensors, int32_t n_tensors,
+                           int32_t cuda_device);
+
+/* out[t] = O(in[t]), without momentum, factor or learning rate.
+ *   in / out   host arrays of n_tensors DEVICE pointers of in_dtype / out_dtype (demo_dtype); out[t] may be in[t] itself if the types agree
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype), CUDA. */
+demo_status demo_orthogonalize(demo_muon_ctx *ctx, const void *const *in, int32_t in_dtype, void *const *out, int32_t out_dtype,
+                               void *cuda_stream);
+
+/* One optimizer step: m <- mu m + g;  U = g + mu m or m;  x <- x - lr (s O(U) + weight_decay x).
+ *   grads      host array of n_tensors DEVICE pointers (cfg.grad_dtype), read-only
+ *   momentum   host array of n_tensors DEVICE pointers (fp32), updated in place
+ *   params     host array of n_tensors DEVICE pointers (fp32), updated in place
+ * Errors: INVALID_ARG, CUDA. */
+demo_status demo_muon_step(demo_muon_ctx *ctx, const void *const *grads, float *const *momentum, float *const *params, void *cuda_stream);
+
+/* demo_decode_apply with an orthogonalised update: R = IDCT(S) as there (demo's aggregation, basis and kernels), then
+ *     2-D tensors   x <- x - lr (s O(R) + weight_decay x)       lr, weight_decay, s of the demo_muon_ctx
+ *     1-D tensors   x <- x - lr (phi(R) + weight_decay x)       all of demo's own
+ * demo's 2-D tensors, in order, have to be those of ctx (SHAPE otherwise), on the same device; contexts of demo_init_nd that keep
+ * rectangular chunks are UNSUPPORTED.  Calls of both contexts are ordered with it.  Its first call allocates 4 bytes for each 2-D
+ * parameter and cannot be part of a stream capture.
+ *   payloads / n_payloads   as in demo_decode_apply
+ *   params                  host array of demo's n_tensors DEVICE pointers (fp32), updated in place
+ * Records with an index outside their chunk are skipped and reported by demo_device_status(demo).
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALLOC, CUDA. */
+demo_status demo_muon_decode_apply(demo_muon_ctx *ctx, demo_ctx *demo, const void *const *payloads, int32_t n_payloads, float *const *params,
+                                   void *cuda_stream);
+
+/* Takes effect for the next call.  Errors: INVALID_ARG (null ctx, non-finite lr). */
+demo_status demo_muon_set_lr(demo_muon_ctx *ctx, float lr);
+/* Bytes of device memory that the context holds, tables and workspace.  0 if ctx is NULL. */
+size_t demo_muon_workspace_bytes(const demo_muon_ctx *ctx);
+/* As demo_launch_count, demo_device_status (DEMO_OK or DEMO_ERR_TIMEOUT) and demo_free. */
+int64_t demo_muon_launch_count(const demo_muon_ctx *ctx);
+demo_status demo_muon_device_status(demo_muon_ctx *ctx, void *cuda_stream);
+void demo_muon_free(demo_muon_ctx *ctx);
+
+/*
+ * AdamW for the tensors that are not orthogonalised (embeddings, output heads, norm vectors): all of them in one launch,
+ *     m <- beta1 m + (1 - beta1) g;   v <- beta2 v + (1 - beta2) g^2
+ *     x <- x - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay x)
+ * with t = *step + 1.  Moments and parameters are fp32.  The rules on buffers, streams, pointer tables and captured graphs are those of
+ * demo_muon_ctx.
+ *   numels     host array: elements of each tensor (1 .. 2^40; order and shape do not matter)
+ *   exp_avg / exp_avg_sq / params   host arrays of n_tensors DEVICE pointers (fp32), updated in place
+ *   step       DEVICE pointer to the number of steps made so far, the caller's, 8-byte aligned; one more afterwards.  Contexts may share
+ *              it only in separate steps: every call moves it on.
+ * Errors: INVALID_ARG (nulls, alignment, 0 <= beta < 1, eps >= 0, values not finite), SHAPE (numels), UNSUPPORTED (dtype, more than 2^20
+ * tensors), ALLOC, CUDA.
+ */
+typedef struct demo_adamw_ctx demo_adamw_ctx; /* opaque, library-owned */
+typedef struct {
+    double beta1, beta2;
+    float eps, lr, weight_decay;
+    int32_t grad_dtype; /* demo_dtype */
+} demo_adamw_config;
+demo_status demo_adamw_init(demo_adamw_ctx **out, const demo_adamw_config *cfg, const int64_t *numels, int32_t n_tensors, int32_t cuda_device);
+demo_status demo_adamw_step(demo_adamw_ctx *ctx, const void *const *grads, float *const *exp_avg, float *const *exp_avg_sq, float *const *params,
+                            int64_t *step, void *cuda_stream);
+demo_status demo_adamw_set_lr(demo_adamw_ctx *ctx, float lr);
+int64_t demo_adamw_launch_count(const demo_adamw_ctx *ctx);
+void demo_adamw_free(demo_adamw_ctx *ctx);
+
 /* Number of kernel launches this context has enqueued since demo_init (for accounting). */
 int64_t demo_launch_count(const demo_ctx *ctx);
 

@@ -6,6 +6,7 @@ This package only marshals arguments: every step of the path runs in the library
 # ``paper_2411_19870_b200.distributed`` (one worker per rank, all-gather of the payloads) is imported on
 # demand: it needs ``torch.distributed``.
 from .binding import (  # noqa: F401
+    AdamwTransform,
     DEMO_BF16,
     DEMO_F32,
     DEMO_AGG_COUNT_MEAN,
@@ -17,10 +18,14 @@ from .binding import (  # noqa: F401
     DEMO_PHI_IDENTITY,
     DEMO_PHI_SIGN,
     DEMO_PATH_GENERIC,
+    DEMO_SCALE_ASPECT,
+    DEMO_SCALE_NONE,
+    DEMO_SCALE_RMS,
     DemoConfig,
     DemoError,
     DemoTensorDesc,
     DemoTransform,
+    MuonTransform,
     RECORD_BYTES,
     decode_apply_static,
     demo_status_string,

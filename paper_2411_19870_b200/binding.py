@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import math
 import os
 from typing import List, Optional, Sequence
 
@@ -23,6 +24,7 @@ DEMO_PATH_AUTO, DEMO_PATH_GENERIC = 0, 1
 DEMO_MOMENTUM_SPATIAL, DEMO_MOMENTUM_DCT = 0, 1
 DEMO_AGG_SUM, DEMO_AGG_MEAN, DEMO_AGG_COUNT_MEAN = 0, 1, 2
 DEMO_PHI_SIGN, DEMO_PHI_IDENTITY = 0, 1
+DEMO_SCALE_NONE, DEMO_SCALE_ASPECT, DEMO_SCALE_RMS = 0, 1, 2
 RECORD_BYTES = 8
 
 EXPORTS = [
@@ -31,6 +33,9 @@ EXPORTS = [
     "demo_step_host", "demo_decode_apply_static", "demo_set_lr", "demo_set_alpha", "demo_set_decode_mode", "demo_set_basis",
     "demo_set_basis_gaussian", "demo_get_basis", "demo_selftest_bounded_wait", "demo_set_path", "demo_set_momentum_domain", "demo_launch_count", "demo_device_status",
     "demo_status_string", "demo_free",
+    "demo_muon_init", "demo_orthogonalize", "demo_muon_step", "demo_muon_decode_apply", "demo_muon_set_lr", "demo_muon_workspace_bytes",
+    "demo_muon_launch_count", "demo_muon_device_status", "demo_muon_free",
+    "demo_adamw_init", "demo_adamw_step", "demo_adamw_set_lr", "demo_adamw_launch_count", "demo_adamw_free",
 ]
 
 
@@ -49,6 +54,21 @@ class DemoConfig(ctypes.Structure):
     _fields_ = [
         ("beta", ctypes.c_float), ("chunk", ctypes.c_int32), ("topk", ctypes.c_int32), ("lr", ctypes.c_float),
         ("weight_decay", ctypes.c_float), ("num_workers", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+    ]
+
+
+class DemoMuonConfig(ctypes.Structure):
+    _fields_ = [
+        ("momentum", ctypes.c_float), ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32), ("coefficients", ctypes.c_float * 3),
+        ("eps", ctypes.c_float), ("lr", ctypes.c_float), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+    ]
+
+
+class DemoAdamwConfig(ctypes.Structure):
+    _fields_ = [
+        ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_float), ("lr", ctypes.c_float),
+        ("weight_decay", ctypes.c_float), ("grad_dtype", ctypes.c_int32),
     ]
 
 
@@ -122,6 +142,34 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.demo_status_string.restype = ctypes.c_char_p
     lib.demo_free.argtypes = [vp]
     lib.demo_free.restype = None
+    lib.demo_muon_init.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(DemoMuonConfig), ctypes.POINTER(DemoTensorDesc), i32, i32]
+    lib.demo_muon_init.restype = i32
+    lib.demo_orthogonalize.argtypes = [vp, pvp, i32, pvp, i32, vp]
+    lib.demo_orthogonalize.restype = i32
+    lib.demo_muon_step.argtypes = [vp, pvp, pvp, pvp, vp]
+    lib.demo_muon_step.restype = i32
+    lib.demo_muon_decode_apply.argtypes = [vp, vp, pvp, i32, pvp, vp]
+    lib.demo_muon_decode_apply.restype = i32
+    lib.demo_muon_set_lr.argtypes = [vp, ctypes.c_float]
+    lib.demo_muon_set_lr.restype = i32
+    lib.demo_muon_workspace_bytes.argtypes = [vp]
+    lib.demo_muon_workspace_bytes.restype = ctypes.c_size_t
+    lib.demo_muon_launch_count.argtypes = [vp]
+    lib.demo_muon_launch_count.restype = i64
+    lib.demo_muon_device_status.argtypes = [vp, vp]
+    lib.demo_muon_device_status.restype = i32
+    lib.demo_muon_free.argtypes = [vp]
+    lib.demo_muon_free.restype = None
+    lib.demo_adamw_init.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(DemoAdamwConfig), ctypes.POINTER(i64), i32, i32]
+    lib.demo_adamw_init.restype = i32
+    lib.demo_adamw_step.argtypes = [vp, pvp, pvp, pvp, pvp, vp, vp]
+    lib.demo_adamw_step.restype = i32
+    lib.demo_adamw_set_lr.argtypes = [vp, ctypes.c_float]
+    lib.demo_adamw_set_lr.restype = i32
+    lib.demo_adamw_launch_count.argtypes = [vp]
+    lib.demo_adamw_launch_count.restype = i64
+    lib.demo_adamw_free.argtypes = [vp]
+    lib.demo_adamw_free.restype = None
     # addresses of the per-step calls, for csrc/calls.cpp
     lib.entry_points = {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value
                         for n in ("demo_compress", "demo_decode_apply", "demo_decode_signs", "demo_apply_signs")}
@@ -446,6 +494,149 @@ class DemoTransform:
     def close(self) -> None:
         if getattr(self, "_ctx", None) is not None and self._ctx.value:
             self.lib.demo_free(self._ctx)
+            self._ctx = ctypes.c_void_p()
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_DTYPES = {torch.float32: DEMO_F32, torch.bfloat16: DEMO_BF16}
+
+
+def _checked(tensors, shapes, dtype, device: int, what: str):
+    """The tensors' addresses for the library, after the checks of ``validate_tensors``."""
+    tensors = list(tensors)
+    validate_tensors(tensors, shapes, dtype, device, what)
+    return _ptr_array(_tensor_ptrs(tensors))
+
+
+class MuonTransform:
+    """One ``demo_muon_ctx``: orthogonalised updates of the matrices with these ``shapes`` (see include/demo.h).  Tensors that are not
+    matrices, and embeddings and heads, go to ``AdamwTransform``."""
+
+    def __init__(self, shapes, *, lr: float, weight_decay: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
+                 coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: int = DEMO_SCALE_RMS, grad_dtype: int = DEMO_BF16,
+                 device: int = 0):
+        self.lib = load_library()
+        self._ctx = ctypes.c_void_p()
+        self.shapes = [tuple(int(d) for d in s) for s in shapes]
+        if len(coefficients) != 3:
+            raise ValueError("coefficients: expected (a, b, c)")
+        self.cfg = DemoMuonConfig(momentum, int(nesterov), steps, (ctypes.c_float * 3)(*coefficients), eps, lr, weight_decay, scale,
+                                  grad_dtype)
+        self.device = device
+        descs = (DemoTensorDesc * len(self.shapes))()
+        for d, s in zip(descs, self.shapes):
+            d.ndim = len(s)
+            for a in range(min(len(s), 2)):
+                d.shape[a] = s[a]
+        st = self.lib.demo_muon_init(ctypes.byref(self._ctx), ctypes.byref(self.cfg), descs, len(self.shapes), device)
+        if st != 0:
+            self._ctx = ctypes.c_void_p()
+            raise DemoError(st, "demo_muon_init")
+        self._grad = torch.bfloat16 if grad_dtype == DEMO_BF16 else torch.float32
+
+    def orthogonalize(self, inputs, outputs, stream=None) -> None:
+        """``outputs[t] = O(inputs[t])``; inputs of one type, outputs of one type, each fp32 or bf16."""
+        inputs, outputs = list(inputs), list(outputs)
+        for what, ts in (("inputs", inputs), ("outputs", outputs)):
+            if not ts or ts[0].dtype not in _DTYPES:
+                raise ValueError("%s: expected fp32 or bf16 tensors" % what)
+        st = self.lib.demo_orthogonalize(self._ctx, _checked(inputs, self.shapes, inputs[0].dtype, self.device, "inputs"),
+                                         _DTYPES[inputs[0].dtype],
+                                         _checked(outputs, self.shapes, outputs[0].dtype, self.device, "outputs"),
+                                         _DTYPES[outputs[0].dtype], DemoTransform._stream(stream))
+        if st != 0:
+            raise DemoError(st, "demo_orthogonalize")
+
+    def step(self, grads, momentum, params, stream=None) -> None:
+        st = self.lib.demo_muon_step(self._ctx, _checked(grads, self.shapes, self._grad, self.device, "grads"),
+                                     _checked(momentum, self.shapes, torch.float32, self.device, "momentum"),
+                                     _checked(params, self.shapes, torch.float32, self.device, "params"), DemoTransform._stream(stream))
+        if st != 0:
+            raise DemoError(st, "demo_muon_step")
+
+    def decode_apply(self, demo: DemoTransform, payloads, params, stream=None) -> None:
+        """``demo.decode_apply`` with orthogonalised updates of its matrices, which are those of this context; ``params``: all of ``demo``'s."""
+        payloads = list(payloads)
+        demo._check_payloads(payloads)
+        st = self.lib.demo_muon_decode_apply(self._ctx, demo._ctx, _ptr_array(_tensor_ptrs(payloads)), len(payloads),
+                                             _checked(params, demo.shapes, torch.float32, self.device, "params"),
+                                             DemoTransform._stream(stream))
+        if st != 0:
+            raise DemoError(st, "demo_muon_decode_apply")
+
+    def set_lr(self, lr: float) -> None:
+        st = self.lib.demo_muon_set_lr(self._ctx, lr)
+        if st != 0:
+            raise DemoError(st, "demo_muon_set_lr")
+
+    @property
+    def workspace_bytes(self) -> int:
+        return int(self.lib.demo_muon_workspace_bytes(self._ctx))
+
+    @property
+    def launch_count(self) -> int:
+        return int(self.lib.demo_muon_launch_count(self._ctx))
+
+    def device_status(self, stream=None) -> int:
+        return int(self.lib.demo_muon_device_status(self._ctx, DemoTransform._stream(stream)))
+
+    def close(self) -> None:
+        if getattr(self, "_ctx", None) is not None and self._ctx.value:
+            self.lib.demo_muon_free(self._ctx)
+            self._ctx = ctypes.c_void_p()
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamwTransform:
+    """One ``demo_adamw_ctx``: the AdamW step of tensors of any ``shapes`` in one launch (see include/demo.h)."""
+
+    def __init__(self, shapes, *, lr: float, weight_decay: float, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
+                 grad_dtype: int = DEMO_BF16, device: int = 0):
+        self.lib = load_library()
+        self._ctx = ctypes.c_void_p()
+        self.shapes = [tuple(int(d) for d in s) for s in shapes]
+        self.cfg = DemoAdamwConfig(beta1, beta2, eps, lr, weight_decay, grad_dtype)
+        self.device = device
+        numels = (ctypes.c_int64 * len(self.shapes))(*[math.prod(s) for s in self.shapes])
+        st = self.lib.demo_adamw_init(ctypes.byref(self._ctx), ctypes.byref(self.cfg), numels, len(self.shapes), device)
+        if st != 0:
+            self._ctx = ctypes.c_void_p()
+            raise DemoError(st, "demo_adamw_init")
+        self._grad = torch.bfloat16 if grad_dtype == DEMO_BF16 else torch.float32
+
+    def step(self, grads, exp_avg, exp_avg_sq, params, step: torch.Tensor, stream=None) -> None:
+        """``step``: int64 tensor of one element on the device, the number of steps made so far; this call adds one."""
+        if step.dtype != torch.int64 or step.numel() != 1 or not step.is_cuda or step.device.index != self.device:
+            raise ValueError("step: need an int64 tensor of one element on cuda:%d" % self.device)
+        lists = [_checked(t, self.shapes, d, self.device, w) for t, d, w in (
+            (grads, self._grad, "grads"), (exp_avg, torch.float32, "exp_avg"), (exp_avg_sq, torch.float32, "exp_avg_sq"),
+            (params, torch.float32, "params"))]
+        st = self.lib.demo_adamw_step(self._ctx, *lists, ctypes.c_void_p(step.data_ptr()), DemoTransform._stream(stream))
+        if st != 0:
+            raise DemoError(st, "demo_adamw_step")
+
+    def set_lr(self, lr: float) -> None:
+        st = self.lib.demo_adamw_set_lr(self._ctx, lr)
+        if st != 0:
+            raise DemoError(st, "demo_adamw_set_lr")
+
+    @property
+    def launch_count(self) -> int:
+        return int(self.lib.demo_adamw_launch_count(self._ctx))
+
+    def close(self) -> None:
+        if getattr(self, "_ctx", None) is not None and self._ctx.value:
+            self.lib.demo_adamw_free(self._ctx)
             self._ctx = ctypes.c_void_p()
 
     def __del__(self):  # pragma: no cover

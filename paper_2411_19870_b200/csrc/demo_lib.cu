@@ -10,6 +10,7 @@
 
 #include "../../include/demo.h"
 #include "demo_internal.h"
+#include "host_common.h"
 #include "launch.cuh"
 
 struct demo_ctx {
@@ -58,6 +59,9 @@ struct demo_ctx {
     float **d_x = nullptr;           // [T]
     const DemoRecord **d_p = nullptr;  // [W]
     signed char **d_s = nullptr;       // [T] sign tensors of the parameter-server form
+    float **d_r = nullptr;             // [T] where demo_decode_momentum writes
+    std::vector<float *> h_r;
+    bool r_valid = false;
     std::vector<signed char *> h_s;
     bool s_valid = false;
     DemoFlatEntry *d_flat = nullptr;   // [T] element ranges for demo_apply_signs
@@ -93,38 +97,6 @@ cudaError_t make_tickets(demo_ctx *c)
     return err == cudaSuccess ? cudaMemset(c->d_tickets, 0, bytes) : err;
 }
 DemoTickets *tickets_of(const demo_ctx *c, int row) { return c->d_tickets + (size_t)row * (size_t)c->ticket_slots; }
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false, changed = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) return;
-        changed = prev != dev;
-        ok = !changed || cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard()
-    {
-        if (ok && changed) cudaSetDevice(prev);
-    }
-};
-
-// Upload `n` pointers to dev[0..n) if they differ from the mirror.  The mirror is pageable host
-// memory: cudaMemcpyAsync stages it before returning, so it may be overwritten by the next call.
-template <typename T>
-cudaError_t sync_table(T *dev, T *mirror, const T *now, int n, bool *valid, cudaStream_t stream,
-                       bool *changed = nullptr)
-{
-    if (changed) *changed = false;
-    if (*valid && std::memcmp(mirror, now, sizeof(T) * (size_t)n) == 0) return cudaSuccess;
-    if (changed) *changed = true;
-    std::memcpy(mirror, now, sizeof(T) * (size_t)n);
-    cudaError_t err = cudaMemcpyAsync(dev, mirror, sizeof(T) * (size_t)n, cudaMemcpyHostToDevice, stream);
-    *valid = (err == cudaSuccess);
-    return err;
-}
 
 // Encode one tensor map per 2-D tensor (box = s x s tile of `elem`-byte elements) for the given base
 // pointers and upload them to dev[0..T).  Returns false if the driver rejects a descriptor.
@@ -168,6 +140,7 @@ void release(demo_ctx *c)
     cudaFree((void *)c->d_x);
     cudaFree((void *)c->d_p);
     cudaFree((void *)c->d_s);
+    cudaFree((void *)c->d_r);
     cudaFree(c->d_flat);
     cudaFree(c->d_tm_g);
     cudaFree(c->d_tm_m);
@@ -718,10 +691,10 @@ static demo_status ensure_sign_tables(demo_ctx *ctx)
     return DEMO_OK;
 }
 
-// demo_decode_apply (params != NULL) and demo_decode_signs (signs != NULL) share everything but the last
-// step of the kernels.
+// demo_decode_apply (params != NULL), demo_decode_signs (signs != NULL) and demo_decode_momentum (params: its table, `momentum` != NULL)
+// share everything but the last step of the kernels.
 static demo_status decode_common(demo_ctx *ctx, const void *const *payloads, int32_t n_payloads, float *const *params,
-                                 signed char *const *signs, void *cuda_stream)
+                                 signed char *const *signs, float *momentum, size_t momentum_bytes, void *cuda_stream)
 {
     if (!ctx || !payloads || (!params && !signs)) return DEMO_ERR_INVALID_ARG;
     if (n_payloads != ctx->cfg.num_workers) return DEMO_ERR_INVALID_ARG;
@@ -741,10 +714,40 @@ static demo_status decode_common(demo_ctx *ctx, const void *const *payloads, int
         if (st != DEMO_OK) return st;
     }
 
+    if (momentum) {
+        // (tables of its own: those of a captured demo_decode_apply stay as they are)
+        const bool same = ctx->r_valid && ctx->p_valid && std::memcmp(ctx->h_r.data(), params, sizeof(float *) * (size_t)T) == 0 &&
+                          std::memcmp(ctx->h_p.data(), payloads, sizeof(void *) * (size_t)W) == 0;
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        if (!same && cudaStreamIsCapturing(stream, &capture) != cudaSuccess) {
+            cudaGetLastError();
+            return DEMO_ERR_CUDA;
+        }
+        if (capture != cudaStreamCaptureStatusNone) return DEMO_ERR_INVALID_ARG;
+        if (!ctx->d_r) {
+            try {
+                ctx->h_r.assign((size_t)T, nullptr);
+            } catch (const std::bad_alloc &) {
+                return DEMO_ERR_ALLOC;
+            }
+            if (cudaMalloc((void **)&ctx->d_r, (size_t)T * sizeof(void *)) != cudaSuccess) {
+                cudaGetLastError();
+                return DEMO_ERR_ALLOC;
+            }
+        }
+        // the kernels add R to what is there
+        if (cudaMemsetAsync(momentum, 0, momentum_bytes, stream) != cudaSuccess) {
+            cudaGetLastError();
+            return DEMO_ERR_CUDA;
+        }
+    }
+
     cudaError_t err = sync_table<const DemoRecord *>(ctx->d_p, ctx->h_p.data(),
                                                      reinterpret_cast<const DemoRecord *const *>(payloads), W,
                                                      &ctx->p_valid, stream);
-    if (err == cudaSuccess && params)
+    if (err == cudaSuccess && momentum)
+        err = sync_table<float *>(ctx->d_r, ctx->h_r.data(), params, T, &ctx->r_valid, stream);
+    else if (err == cudaSuccess && params)
         err = sync_table<float *>(ctx->d_x, ctx->h_x.data(), const_cast<float *const *>(params), T, &ctx->x_valid,
                                   stream);
     if (err == cudaSuccess && signs)
@@ -785,7 +788,7 @@ static demo_status decode_common(demo_ctx *ctx, const void *const *payloads, int
     DemoDecodeArgs a;
     a.payloads = ctx->d_p;
     a.W = W;
-    a.x_ptrs = ctx->d_x;
+    a.x_ptrs = momentum ? ctx->d_r : ctx->d_x;
     a.C = ctx->custom_basis ? ctx->d_P : ctx->d_C;
     a.lr = ctx->cfg.lr;
     a.wd = ctx->cfg.weight_decay;
@@ -804,6 +807,11 @@ static demo_status decode_common(demo_ctx *ctx, const void *const *payloads, int
     a.n_chunks = ctx->chunks2d;
     a.k = ctx->cfg.topk;  // <= s * s
     a.tickets = tickets_of(ctx, W);
+    if (momentum) {  // 0 - (-1) (R + 0)
+        a.phi = DEMO_PHI_IDENTITY;
+        a.lr = -1.0f;
+        a.wd = 0.0f;
+    }
     const bool small_tiles = ctx->n2d && use_small_tiles_decode(ctx);
     if (ctx->n2d && !small_tiles) {
         // (a caller-supplied basis: the signs come from the dense kernels, there is no tensor-core variant)
@@ -832,14 +840,14 @@ demo_status demo_decode_apply(demo_ctx *ctx, const void *const *payloads, int32_
                               void *cuda_stream)
 {
     if (!params) return DEMO_ERR_INVALID_ARG;
-    return decode_common(ctx, payloads, n_payloads, params, nullptr, cuda_stream);
+    return decode_common(ctx, payloads, n_payloads, params, nullptr, nullptr, 0, cuda_stream);
 }
 
 demo_status demo_decode_signs(demo_ctx *ctx, const void *const *payloads, int32_t n_payloads, int8_t *const *signs_out,
                               void *cuda_stream)
 {
     if (!signs_out) return DEMO_ERR_INVALID_ARG;
-    return decode_common(ctx, payloads, n_payloads, nullptr, reinterpret_cast<signed char *const *>(signs_out),
+    return decode_common(ctx, payloads, n_payloads, nullptr, reinterpret_cast<signed char *const *>(signs_out), nullptr, 0,
                          cuda_stream);
 }
 
@@ -1110,3 +1118,26 @@ void demo_free(demo_ctx *ctx)
 }
 
 }  // extern "C"
+
+demo_status demo_decode_places(const demo_ctx *ctx, int device, const demo_tensor_desc *matrices, int n, std::vector<int> *place)
+{
+    if (ctx->nd) return DEMO_ERR_UNSUPPORTED;
+    if (ctx->device != device) return DEMO_ERR_INVALID_ARG;
+    place->clear();
+    int next = 0;
+    for (const demo_tensor_desc &d : ctx->descs) {
+        if (d.ndim != 2) {
+            place->push_back(-1);
+            continue;
+        }
+        if (next == n || d.shape[0] != matrices[next].shape[0] || d.shape[1] != matrices[next].shape[1]) return DEMO_ERR_SHAPE;
+        place->push_back(next++);
+    }
+    return next == n ? DEMO_OK : DEMO_ERR_SHAPE;
+}
+
+demo_status demo_decode_momentum(demo_ctx *ctx, const void *const *payloads, int32_t n_payloads, float *const *to, float *momentum,
+                                 size_t momentum_bytes, cudaStream_t stream)
+{
+    return decode_common(ctx, payloads, n_payloads, to, nullptr, momentum, momentum_bytes, stream);
+}

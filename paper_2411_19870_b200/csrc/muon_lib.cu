@@ -1,0 +1,501 @@
+// Host side of the orthogonalised updates in include/demo.h: plan (groups of matrices, tiles), workspace and tensor maps, launches.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "../../include/demo.h"
+#include "demo_internal.h"
+#include "host_common.h"
+#include "launch.cuh"
+#include "muon.h"
+
+namespace {
+
+// Matrices that go through the iterations together: one launch for each product of all of them.
+struct Group {
+    int first_mat, n_mats, n_pieces;
+    bool pair;  // tiles of 256 x 256
+    long long pack_tiles, sym_tiles, full_tiles;  // first of each list
+    int n_pack, n_sym, n_full;
+};
+
+// Pointer arrays of an entry point: device table and mirror, uploaded when they change.
+struct Tables {
+    const void **d_in = nullptr;
+    float **d_mom = nullptr;
+    void **d_out = nullptr;
+    std::vector<const void *> in;
+    std::vector<float *> mom;
+    std::vector<void *> out;
+    bool valid = false;
+};
+enum { FROM_ORTHOGONALIZE = 0, FROM_STEP = 1, FROM_DECODE = 2, ENTRY_POINTS = 3 };
+
+constexpr long long GROUP_ELEMENTS = 32LL << 20;  // workspace: 8 bytes for each, and A and F beside them
+constexpr int PRECISE_SIDE = 256;                 // up to here the products take the lo parts, too (kernels_muon.cu)
+
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+}  // namespace
+
+struct demo_muon_ctx {
+    demo_muon_config cfg;
+    int device = 0, n_tensors = 0;
+    DemoLaunch launch;
+    std::vector<demo_tensor_desc> descs;
+    std::vector<Group> groups;
+    long long launches = 0;
+    size_t bytes = 0;
+    MuonMat *d_mats = nullptr;
+    MuonTile *d_tiles = nullptr;
+    char *d_maps = nullptr;
+    char *d_work = nullptr;
+    double *d_partials = nullptr;
+    int *d_status = nullptr;
+    Tables tables[ENTRY_POINTS];
+    float *d_momentum = nullptr;  // reconstructed momenta of demo_muon_decode_apply, from its first call
+    size_t momentum_bytes = 0;
+    std::vector<float *> momentum_ptrs;
+};
+
+namespace {
+
+void release(demo_muon_ctx *c)
+{
+    if (!c) return;
+    cudaFree(c->d_mats);
+    cudaFree(c->d_tiles);
+    cudaFree(c->d_maps);
+    cudaFree(c->d_work);
+    cudaFree(c->d_partials);
+    cudaFree(c->d_status);
+    cudaFree(c->d_momentum);
+    for (Tables &t : c->tables) {
+        cudaFree((void *)t.d_in);
+        cudaFree((void *)t.d_mom);
+        cudaFree((void *)t.d_out);
+    }
+    delete c;
+}
+
+struct Plan {
+    std::vector<MuonMat> mats;
+    std::vector<MuonTile> tiles;
+    size_t work = 0;
+    int pieces = 0;
+};
+
+// Workspace of one matrix from `at` on, as offsets (the base is added once it is known).  Returns its end.
+size_t place(MuonMat &m, size_t at)
+{
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (size_t)round_up((long long)bytes, 256);
+        return reinterpret_cast<uint16_t *>(here);
+    };
+    const size_t x = (size_t)m.m * (size_t)m.ldx * 2, e = (size_t)m.m * (size_t)m.lde * 2;
+    for (int p = 0; p < 2; ++p) m.xhi[p] = take(x), m.xlo[p] = take(x);
+    m.ehi = take(e);
+    m.fhi = take(e);
+    m.elo = m.precise ? take(e) : m.ehi;
+    m.flo = m.precise ? take(e) : m.fhi;
+    m.d = reinterpret_cast<float *>(take((size_t)m.m * 4));
+    m.beta = reinterpret_cast<float *>(take((size_t)m.m * 4));
+    return at;
+}
+void rebase(MuonMat &m, char *base)
+{
+    auto move = [&](auto *&p) { p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + reinterpret_cast<size_t>(p)); };
+    for (int p = 0; p < 2; ++p) {
+        move(m.xhi[p]);
+        move(m.xlo[p]);
+    }
+    move(m.ehi);
+    move(m.elo);
+    move(m.fhi);
+    move(m.flo);
+    move(m.d);
+    move(m.beta);
+}
+
+bool uses_pairs(const MuonMat &m) { return m.m > PRECISE_SIDE; }
+
+demo_status make_plan(demo_muon_ctx *c, Plan *plan)
+{
+    std::vector<MuonMat> all((size_t)c->n_tensors);
+    for (int t = 0; t < c->n_tensors; ++t) {
+        MuonMat &m = all[(size_t)t];
+        std::memset(&m, 0, sizeof(m));
+        const long long rows = c->descs[(size_t)t].shape[0], cols = c->descs[(size_t)t].shape[1];
+        m.transposed = rows > cols;
+        m.m = (int)std::min(rows, cols);
+        m.n = (int)std::max(rows, cols);
+        m.ldx = (int)round_up(m.n, 64);
+        m.lde = (int)round_up(m.m, 64);
+        m.precise = m.m <= PRECISE_SIDE;
+        m.tensor = t;
+        // X's elements are of order one once its singular values are: then neither hi nor lo leaves the normal range of fp16
+        m.S = (float)std::exp2(std::floor(0.5 * std::log2((double)m.n)));
+        m.inv_S = 1.0f / m.S;
+        m.step_scale = c->cfg.scale == DEMO_SCALE_RMS      ? 0.2f * std::sqrt((float)m.n)
+                       : c->cfg.scale == DEMO_SCALE_ASPECT ? std::sqrt(std::max(1.0f, (float)rows / (float)cols))
+                                                           : 1.0f;
+    }
+    // groups hold matrices of one kind of tile
+    std::stable_sort(all.begin(), all.end(), [](const MuonMat &x, const MuonMat &y) { return uses_pairs(x) > uses_pairs(y); });
+    for (size_t at = 0; at < all.size();) {
+        Group g;
+        std::memset(&g, 0, sizeof(g));
+        g.first_mat = (int)at;
+        g.pair = uses_pairs(all[at]);
+        long long elements = 0, pieces = 0;
+        size_t work = 0, end = at;
+        for (; end < all.size() && uses_pairs(all[end]) == g.pair; ++end) {
+            MuonMat &m = all[end];
+            const long long n = (long long)m.m * m.n;
+            if (end > at && elements + n > GROUP_ELEMENTS) break;
+            elements += n;
+            m.piece_begin = (int)pieces;
+            m.n_pieces = (int)((n + MUON_PIECE - 1) / MUON_PIECE);
+            pieces += m.n_pieces;
+            work = place(m, work);
+            m.maps = (int)end * MUON_MAPS;
+        }
+        if (pieces > (1LL << 31) - 1) return DEMO_ERR_UNSUPPORTED;
+        g.n_mats = (int)(end - at);
+        g.n_pieces = (int)pieces;
+        plan->work = std::max(plan->work, work);
+        plan->pieces = std::max(plan->pieces, g.n_pieces);
+        const int side = g.pair ? 256 : 128;
+        auto grid = [&](int tile_m, int tile_n, bool upper, bool square, long long *first, int *count) {
+            *first = (long long)plan->tiles.size();
+            for (size_t e = at; e < end; ++e) {
+                const MuonMat &m = all[e];
+                const int ni = (m.m + tile_m - 1) / tile_m, nj = ((square ? m.m : m.n) + tile_n - 1) / tile_n;
+                for (int i = 0; i < ni; ++i)
+                    for (int j = upper ? i : 0; j < nj; ++j) plan->tiles.push_back(MuonTile{(int)e, (short)i, (short)j});
+            }
+            *count = (int)((long long)plan->tiles.size() - *first);
+        };
+        grid(MUON_PACK_TILE, MUON_PACK_TILE, false, false, &g.pack_tiles, &g.n_pack);
+        grid(side, side, true, true, &g.sym_tiles, &g.n_sym);
+        grid(side, side, false, false, &g.full_tiles, &g.n_full);
+        if (plan->tiles.size() > (size_t)(1LL << 31) - 1) return DEMO_ERR_UNSUPPORTED;
+        c->groups.push_back(g);
+        at = end;
+    }
+    plan->mats = std::move(all);
+    return DEMO_OK;
+}
+
+bool encode_map(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, void *base, long long cols, long long rows, long long ld)
+{
+    const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t gstride[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {64, 64}, estr[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T>
+bool alloc(demo_muon_ctx *c, T **p, size_t bytes)
+{
+    if (cudaMalloc((void **)p, bytes) != cudaSuccess) return false;
+    c->bytes += bytes;
+    return true;
+}
+
+demo_status build(demo_muon_ctx *c)
+{
+    Plan plan;
+    demo_status st = make_plan(c, &plan);
+    if (st != DEMO_OK) return st;
+    PFN_cuTensorMapEncodeTiled encode = nullptr;
+    {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
+            return DEMO_ERR_UNSUPPORTED;
+        encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled>(fn);
+    }
+    const size_t T = (size_t)c->n_tensors;
+    bool ok = alloc(c, &c->d_mats, T * sizeof(MuonMat)) && alloc(c, &c->d_tiles, plan.tiles.size() * sizeof(MuonTile)) &&
+              alloc(c, &c->d_maps, T * MUON_MAPS * MUON_MAP_BYTES) && alloc(c, &c->d_work, plan.work) &&
+              alloc(c, &c->d_partials, (size_t)plan.pieces * sizeof(double)) && alloc(c, &c->d_status, sizeof(int));
+    for (Tables &t : c->tables) {
+        ok = ok && alloc(c, (void **)&t.d_in, T * sizeof(void *)) && alloc(c, (void **)&t.d_mom, T * sizeof(void *)) && alloc(c, (void **)&t.d_out, T * sizeof(void *));
+        t.in.assign(T, nullptr);
+        t.mom.assign(T, nullptr);
+        t.out.assign(T, nullptr);
+    }
+    if (!ok) return DEMO_ERR_ALLOC;
+    std::vector<CUtensorMap> maps(T * MUON_MAPS);
+    std::memset(maps.data(), 0, maps.size() * sizeof(CUtensorMap));
+    for (MuonMat &m : plan.mats) {
+        rebase(m, c->d_work);
+        CUtensorMap *p = &maps[(size_t)m.maps];
+        ok = ok && encode_map(encode, p + MUON_MAP_X0, m.xhi[0], m.n, m.m, m.ldx) && encode_map(encode, p + MUON_MAP_X1, m.xhi[1], m.n, m.m, m.ldx) &&
+             encode_map(encode, p + MUON_MAP_XLO0, m.xlo[0], m.n, m.m, m.ldx) && encode_map(encode, p + MUON_MAP_XLO1, m.xlo[1], m.n, m.m, m.ldx) &&
+             encode_map(encode, p + MUON_MAP_E, m.ehi, m.m, m.m, m.lde) && encode_map(encode, p + MUON_MAP_ELO, m.elo, m.m, m.m, m.lde) &&
+             encode_map(encode, p + MUON_MAP_F, m.fhi, m.m, m.m, m.lde) && encode_map(encode, p + MUON_MAP_FLO, m.flo, m.m, m.m, m.lde);
+    }
+    if (!ok) return DEMO_ERR_CUDA;
+    ok = cudaMemcpy(c->d_mats, plan.mats.data(), T * sizeof(MuonMat), cudaMemcpyHostToDevice) == cudaSuccess &&
+         cudaMemcpy(c->d_tiles, plan.tiles.data(), plan.tiles.size() * sizeof(MuonTile), cudaMemcpyHostToDevice) == cudaSuccess &&
+         cudaMemcpy(c->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice) == cudaSuccess &&
+         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess;
+    return ok ? DEMO_OK : DEMO_ERR_CUDA;
+}
+
+// The tables of an entry point for these pointers.  A table that a captured graph would have to copy is refused: the graph would copy
+// whatever the host array holds when it runs.
+demo_status sync_tables(demo_muon_ctx *c, Tables &t, const void *const *in, float *const *mom, void *const *out, cudaStream_t stream)
+{
+    const size_t bytes = (size_t)c->n_tensors * sizeof(void *);
+    if (t.valid && !std::memcmp(t.in.data(), in, bytes) && (!mom || !std::memcmp(t.mom.data(), mom, bytes)) && !std::memcmp(t.out.data(), out, bytes)) return DEMO_OK;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess) {
+        cudaGetLastError();
+        return DEMO_ERR_CUDA;
+    }
+    if (capture != cudaStreamCaptureStatusNone) return DEMO_ERR_INVALID_ARG;
+    t.valid = false;
+    std::memcpy(t.in.data(), in, bytes);
+    if (mom) std::memcpy(t.mom.data(), mom, bytes);
+    std::memcpy(t.out.data(), out, bytes);
+    bool ok = cudaMemcpyAsync(t.d_in, t.in.data(), bytes, cudaMemcpyHostToDevice, stream) == cudaSuccess;
+    ok = ok && (!mom || cudaMemcpyAsync(t.d_mom, t.mom.data(), bytes, cudaMemcpyHostToDevice, stream) == cudaSuccess);
+    ok = ok && cudaMemcpyAsync(t.d_out, t.out.data(), bytes, cudaMemcpyHostToDevice, stream) == cudaSuccess;
+    t.valid = ok;
+    if (!ok) cudaGetLastError();
+    return ok ? DEMO_OK : DEMO_ERR_CUDA;
+}
+
+demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stream)
+{
+    const demo_muon_config &g = c->cfg;
+    a.mats = c->d_mats;
+    a.maps = c->d_maps;
+    a.in = t.d_in;
+    a.mom = t.d_mom;
+    a.out = t.d_out;
+    a.partials = c->d_partials;
+    a.nesterov = g.nesterov;
+    a.mu = g.momentum;
+    a.eps = g.eps;
+    a.lr = g.lr;
+    a.wd = g.weight_decay;
+    a.a = g.coefficients[0];
+    a.b = g.coefficients[1];
+    a.c = g.coefficients[2];
+    a.status = c->d_status;
+    cudaError_t err = cudaSuccess;
+    for (const Group &grp : c->groups) {
+        const MuonTile *pack = c->d_tiles + grp.pack_tiles, *sym = c->d_tiles + grp.sym_tiles, *full = c->d_tiles + grp.full_tiles;
+        if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, stream);
+        if (err == cudaSuccess) err = muon_launch_pack(a, pack, grp.n_pack, c->launch, stream);
+        for (int k = 0; k < g.steps; ++k) {
+            if (err == cudaSuccess) err = muon_launch_product(MUON_GRAM, grp.pair, k & 1, a, sym, grp.n_sym, c->launch, stream);
+            if (err == cudaSuccess) err = muon_launch_product(MUON_POLY, grp.pair, k & 1, a, sym, grp.n_sym, c->launch, stream);
+            if (err == cudaSuccess) err = muon_launch_product(k + 1 < g.steps ? MUON_UPDATE : MUON_FINAL, grp.pair, k & 1, a, full, grp.n_full, c->launch, stream);
+        }
+        c->launches += 2 + 3 * g.steps;
+    }
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        return DEMO_ERR_CUDA;
+    }
+    return DEMO_OK;
+}
+
+bool usable(const void *const *p, int n)
+{
+    for (int t = 0; t < n; ++t)
+        if (!p[t] || !aligned16(p[t])) return false;
+    return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+demo_status demo_muon_init(demo_muon_ctx **out, const demo_muon_config *cfg, const demo_tensor_desc *tensors, int32_t n_tensors, int32_t cuda_device)
+{
+    if (out) *out = nullptr;
+    if (!out || !cfg || !tensors || n_tensors < 1 || cuda_device < 0) return DEMO_ERR_INVALID_ARG;
+    for (const float v : {cfg->momentum, cfg->coefficients[0], cfg->coefficients[1], cfg->coefficients[2], cfg->eps, cfg->lr, cfg->weight_decay})
+        if (!std::isfinite(v)) return DEMO_ERR_INVALID_ARG;
+    if (cfg->steps < 1 || cfg->steps > DEMO_MUON_MAX_STEPS || cfg->eps < 0 || (cfg->nesterov != 0 && cfg->nesterov != 1)) return DEMO_ERR_INVALID_ARG;
+    if (cfg->scale != DEMO_SCALE_NONE && cfg->scale != DEMO_SCALE_ASPECT && cfg->scale != DEMO_SCALE_RMS) return DEMO_ERR_INVALID_ARG;
+    if (cfg->grad_dtype != DEMO_F32 && cfg->grad_dtype != DEMO_BF16) return DEMO_ERR_UNSUPPORTED;
+    if (n_tensors > (1 << 20)) return DEMO_ERR_UNSUPPORTED;
+    for (int t = 0; t < n_tensors; ++t) {
+        const demo_tensor_desc &d = tensors[t];
+        if (d.ndim != 2) return DEMO_ERR_SHAPE;
+        for (int a = 0; a < 2; ++a)
+            if (d.shape[a] < 1 || d.shape[a] > DEMO_MUON_MAX_EXTENT) return DEMO_ERR_SHAPE;
+    }
+    int n_dev = 0;
+    if (cudaGetDeviceCount(&n_dev) != cudaSuccess || cuda_device >= n_dev) {
+        cudaGetLastError();
+        return DEMO_ERR_CUDA;
+    }
+    DeviceGuard guard(cuda_device);
+    if (!guard.ok) return DEMO_ERR_CUDA;
+    demo_muon_ctx *c = new (std::nothrow) demo_muon_ctx();
+    if (!c) return DEMO_ERR_ALLOC;
+    demo_status st = DEMO_OK;
+    if (cudaDeviceGetAttribute(&c->launch.sm_count, cudaDevAttrMultiProcessorCount, cuda_device) != cudaSuccess) st = DEMO_ERR_CUDA;
+    if (st == DEMO_OK) {
+        try {
+            c->cfg = *cfg;
+            c->device = cuda_device;
+            c->n_tensors = n_tensors;
+            c->descs.assign(tensors, tensors + n_tensors);
+            st = build(c);
+        } catch (const std::bad_alloc &) {
+            st = DEMO_ERR_ALLOC;
+        }
+    }
+    if (st != DEMO_OK) {
+        cudaGetLastError();
+        release(c);
+        return st;
+    }
+    *out = c;
+    return DEMO_OK;
+}
+
+demo_status demo_orthogonalize(demo_muon_ctx *ctx, const void *const *in, int32_t in_dtype, void *const *out, int32_t out_dtype, void *cuda_stream)
+{
+    if (!ctx || !in || !out) return DEMO_ERR_INVALID_ARG;
+    for (const int32_t d : {in_dtype, out_dtype})
+        if (d != DEMO_F32 && d != DEMO_BF16) return DEMO_ERR_UNSUPPORTED;
+    if (!usable(in, ctx->n_tensors) || !usable(out, ctx->n_tensors)) return DEMO_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return DEMO_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    Tables &t = ctx->tables[FROM_ORTHOGONALIZE];
+    const demo_status st = sync_tables(ctx, t, in, nullptr, out, stream);
+    if (st != DEMO_OK) return st;
+    MuonArgs a{};
+    a.from = MUON_FROM_INPUT;
+    a.to = MUON_TO_OUTPUT;
+    a.in_bf16 = in_dtype == DEMO_BF16;
+    a.out_bf16 = out_dtype == DEMO_BF16;
+    return run(ctx, a, t, stream);
+}
+
+demo_status demo_muon_step(demo_muon_ctx *ctx, const void *const *grads, float *const *momentum, float *const *params, void *cuda_stream)
+{
+    if (!ctx || !grads || !momentum || !params) return DEMO_ERR_INVALID_ARG;
+    if (!usable(grads, ctx->n_tensors) || !usable(reinterpret_cast<const void *const *>(momentum), ctx->n_tensors) ||
+        !usable(reinterpret_cast<const void *const *>(params), ctx->n_tensors))
+        return DEMO_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return DEMO_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    Tables &t = ctx->tables[FROM_STEP];
+    const demo_status st = sync_tables(ctx, t, grads, momentum, reinterpret_cast<void *const *>(params), stream);
+    if (st != DEMO_OK) return st;
+    MuonArgs a{};
+    a.from = MUON_FROM_STEP;
+    a.to = MUON_TO_PARAMS;
+    a.in_bf16 = ctx->cfg.grad_dtype == DEMO_BF16;
+    return run(ctx, a, t, stream);
+}
+
+demo_status demo_muon_decode_apply(demo_muon_ctx *ctx, demo_ctx *demo, const void *const *payloads, int32_t n_payloads, float *const *params, void *cuda_stream)
+{
+    if (!ctx || !demo || !payloads || !params) return DEMO_ERR_INVALID_ARG;
+    std::vector<void *> out;
+    std::vector<float *> table;
+    try {
+        std::vector<int> place;
+        const demo_status st = demo_decode_places(demo, ctx->device, ctx->descs.data(), ctx->n_tensors, &place);
+        if (st != DEMO_OK) return st;
+        if (!usable(reinterpret_cast<const void *const *>(params), (int)place.size())) return DEMO_ERR_INVALID_ARG;
+        DeviceGuard guard(ctx->device);
+        if (!guard.ok) return DEMO_ERR_CUDA;
+        cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+        if (!ctx->d_momentum) {
+            cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+            if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess) {
+                cudaGetLastError();
+                return DEMO_ERR_CUDA;
+            }
+            if (capture != cudaStreamCaptureStatusNone) return DEMO_ERR_INVALID_ARG;
+            size_t n = 0;
+            for (const demo_tensor_desc &d : ctx->descs) n += (size_t)round_up(d.shape[0] * d.shape[1], 64);
+            ctx->momentum_ptrs.assign((size_t)ctx->n_tensors, nullptr);
+            if (!alloc(ctx, &ctx->d_momentum, n * sizeof(float))) {
+                cudaGetLastError();
+                ctx->d_momentum = nullptr;
+                return DEMO_ERR_ALLOC;
+            }
+            ctx->momentum_bytes = n * sizeof(float);
+            size_t at = 0;
+            for (int t = 0; t < ctx->n_tensors; ++t) {
+                ctx->momentum_ptrs[(size_t)t] = ctx->d_momentum + at;
+                at += (size_t)round_up(ctx->descs[(size_t)t].shape[0] * ctx->descs[(size_t)t].shape[1], 64);
+            }
+        }
+        table.resize(place.size());
+        out.resize((size_t)ctx->n_tensors);
+        for (size_t i = 0; i < place.size(); ++i) {
+            table[i] = place[i] < 0 ? params[i] : ctx->momentum_ptrs[(size_t)place[i]];
+            if (place[i] >= 0) out[(size_t)place[i]] = params[i];
+        }
+        Tables &t = ctx->tables[FROM_DECODE];
+        demo_status done = sync_tables(ctx, t, reinterpret_cast<const void *const *>(ctx->momentum_ptrs.data()), nullptr, out.data(), stream);
+        if (done != DEMO_OK) return done;
+        done = demo_decode_momentum(demo, payloads, n_payloads, table.data(), ctx->d_momentum, ctx->momentum_bytes, stream);
+        if (done != DEMO_OK) return done;
+        MuonArgs a{};
+        a.from = MUON_FROM_INPUT;
+        a.to = MUON_TO_PARAMS;
+        return run(ctx, a, t, stream);
+    } catch (const std::bad_alloc &) {
+        return DEMO_ERR_ALLOC;
+    }
+}
+
+demo_status demo_muon_set_lr(demo_muon_ctx *ctx, float lr)
+{
+    if (!ctx || !std::isfinite(lr)) return DEMO_ERR_INVALID_ARG;
+    ctx->cfg.lr = lr;
+    return DEMO_OK;
+}
+
+size_t demo_muon_workspace_bytes(const demo_muon_ctx *ctx) { return ctx ? ctx->bytes : 0; }
+
+int64_t demo_muon_launch_count(const demo_muon_ctx *ctx) { return ctx ? ctx->launches : 0; }
+
+demo_status demo_muon_device_status(demo_muon_ctx *ctx, void *cuda_stream)
+{
+    if (!ctx) return DEMO_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return DEMO_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    int word = 0;
+    if (cudaMemcpyAsync(&word, ctx->d_status, sizeof(int), cudaMemcpyDeviceToHost, stream) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess ||
+        (word != 0 && (cudaMemsetAsync(ctx->d_status, 0, sizeof(int), stream) != cudaSuccess || cudaStreamSynchronize(stream) != cudaSuccess))) {
+        cudaGetLastError();
+        return DEMO_ERR_CUDA;
+    }
+    return word == 0 ? DEMO_OK : word == DEMO_DEV_TIMEOUT ? DEMO_ERR_TIMEOUT : DEMO_ERR_CUDA;
+}
+
+void demo_muon_free(demo_muon_ctx *ctx)
+{
+    if (!ctx) return;
+    DeviceGuard guard(ctx->device);
+    release(ctx);
+}
+
+}  // extern "C"
