@@ -2,7 +2,7 @@
 //
 //   X_0 = u / (||u||_F + eps);  A = X X^T;  X <- a X + (b A + c A^2) X
 //
-// as three products an iteration, each over all matrices of a group:
+// as three products an iteration, the tasks of one persistent kernel:
 //   GRAM    A = X X^T        symmetric: the tiles on and above the diagonal, mirrored
 //   POLY    A^2 -> F, beta   symmetric, too
 //   UPDATE  F X  -> X
@@ -55,6 +55,7 @@ __device__ __forceinline__ double block_sum(double v, double *scratch)
 {
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_down_sync(0xffffffffu, v, d);
+    __syncthreads();  // (scratch may still be read from the sum before)
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
     __syncthreads();
     double s = 0;
@@ -112,75 +113,143 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_norm_kernel(MuonArgs a, int
         if (mom) mom[at + rest] = m;
     }
     const double s = block_sum(sum, scratch);
-    if (threadIdx.x == 0) a.partials[blockIdx.x] = s;
+    // the matrix's last piece to be ready adds them all up, in one order whichever it is
+    __shared__ int last;
+    if (threadIdx.x == 0) {
+        a.partials[blockIdx.x] = s;
+        __threadfence();
+        last = atomicInc(a.ready + e, (unsigned)mat.n_pieces - 1u) == (unsigned)mat.n_pieces - 1u;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    sum = 0;
+    for (int p = threadIdx.x; p < mat.n_pieces; p += NORM_THREADS) sum += __ldcg(a.partials + mat.piece_begin + p);
+    const double norm = sqrt(block_sum(sum, scratch));
+    if (threadIdx.x == 0) {
+        const double all = norm + (double)a.eps, scale = all > 0 ? (double)mat.S / all : 1;
+        // in two factors, so that neither leaves the range of fp32 where the norm is near its ends
+        const float scale1 = (float)exp2(floor(0.5 * log2(scale)));
+        a.scales[e] = make_float2(scale1, (float)(scale / (double)scale1));
+    }
 }
 
-__device__ __forceinline__ void split(float v, __half &hi, __half &lo)
+__device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+__device__ __forceinline__ uint32_t pack2(float x, float y)
 {
-    hi = __float2half_rn(v);
-    lo = __float2half_rn(v - __half2float(hi));
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// A tile of 64 x 64 elements of X.  The pieces' sums are added in one order by every CTA.
-__global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, const MuonTile *tiles)
+// A tile of 64 x 64 elements of X.
+__global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, const MuonTile *tiles, int first_mat, int n_mats)
 {
     const StreamOrder order(1);
     constexpr int T = MUON_PACK_TILE;
-    __shared__ double scratch[NORM_THREADS / 32];
     __shared__ float tile[T][T + 1];
     const MuonTile t = tiles[blockIdx.x];
     const MuonMat &mat = a.mats[t.mat];
-    order.begin();
-    double sum = 0;
-    for (int p = threadIdx.x; p < mat.n_pieces; p += NORM_THREADS) sum += a.partials[mat.piece_begin + p];
-    const double norm = sqrt(block_sum(sum, scratch));
-    const double all = norm + (double)a.eps, scale_d = all > 0 ? (double)mat.S / all : 1;
-    // in two factors, so that neither leaves the range of fp32 where the norm is near its ends
-    const float scale1 = (float)exp2(floor(0.5 * log2(scale_d))), scale2 = (float)(scale_d / (double)scale1);
-    const void *in = a.in[mat.tensor];
-    const float *mom = a.from == MUON_FROM_STEP ? a.mom[mat.tensor] : nullptr;
-    const int rows = mat.transposed ? mat.n : mat.m, cols = mat.transposed ? mat.m : mat.n;
+    const int transposed = mat.transposed, rows = transposed ? mat.n : mat.m, cols = transposed ? mat.m : mat.n;
     // tile row i0, column j0 of X; of the tensor, the other way round where X is its transpose
     const int i0 = t.i * T, j0 = t.j * T;
-    const int r0 = mat.transposed ? j0 : i0, c0 = mat.transposed ? i0 : j0;
-    const int x = threadIdx.x & (T - 1);
-#pragma unroll 4
-    for (int y = threadIdx.x / T; y < T; y += NORM_THREADS / T) {
-        const int r = r0 + y, c = c0 + x;
-        float u = 0.f;
-        if (r < rows && c < cols) {
-            const long long at = (long long)r * cols + c;
-            u = load_in(in, at, a.in_bf16);
+    const int r0 = transposed ? j0 : i0, c0 = transposed ? i0 : j0;
+    const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;  // four elements of a row, sixteen rows at a time
+    constexpr int ROWS = NORM_THREADS / 16;
+    order.begin();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.next_task = 0;
+    for (int k = blockIdx.x * NORM_THREADS + threadIdx.x; k < n_mats; k += gridDim.x * NORM_THREADS) a.done[first_mat + k] = 0;
+    const void *in = a.in[mat.tensor];
+    const float *mom = a.from == MUON_FROM_STEP ? a.mom[mat.tensor] : nullptr;
+    float u[T / ROWS][4];
+    const bool whole = (cols & 3) == 0;
+#pragma unroll
+    for (int k = 0; k < T / ROWS; ++k) {
+        const int r = r0 + y + k * ROWS, c = c0 + x;
+        const long long at = (long long)r * cols + c;
+        float m[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int l = 0; l < 4; ++l) u[k][l] = 0.f;
+        if (r < rows) {
+            if (whole && c < cols) {
+                if (a.in_bf16) {
+                    const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(in) + at);
+                    u[k][0] = __uint_as_float(v.x << 16);
+                    u[k][1] = __uint_as_float(v.x & 0xffff0000u);
+                    u[k][2] = __uint_as_float(v.y << 16);
+                    u[k][3] = __uint_as_float(v.y & 0xffff0000u);
+                } else {
+                    const float4 v = *reinterpret_cast<const float4 *>(static_cast<const float *>(in) + at);
+                    u[k][0] = v.x, u[k][1] = v.y, u[k][2] = v.z, u[k][3] = v.w;
+                }
+                if (mom) {
+                    const float4 v = *reinterpret_cast<const float4 *>(mom + at);
+                    m[0] = v.x, m[1] = v.y, m[2] = v.z, m[3] = v.w;
+                }
+            } else if (!whole) {
+#pragma unroll
+                for (int l = 0; l < 4; ++l)
+                    if (c + l < cols) {
+                        u[k][l] = load_in(in, at + l, a.in_bf16);
+                        if (mom) m[l] = mom[at + l];
+                    }
+            }
             if (mom) {
-                const float m = mom[at];
-                u = a.nesterov ? fmaf(a.mu, m, u) : m;
+#pragma unroll
+                for (int l = 0; l < 4; ++l) u[k][l] = a.nesterov ? fmaf(a.mu, m[l], u[k][l]) : m[l];
             }
         }
-        tile[y][x] = u * scale1 * scale2;
+    }
+    const float2 scale = a.scales[t.mat];
+#pragma unroll
+    for (int k = 0; k < T / ROWS; ++k)
+#pragma unroll
+        for (int l = 0; l < 4; ++l) u[k][l] = u[k][l] * scale.x * scale.y;
+    if (transposed) {
+#pragma unroll
+        for (int k = 0; k < T / ROWS; ++k)
+#pragma unroll
+            for (int l = 0; l < 4; ++l) tile[x + l][y + k * ROWS] = u[k][l];
+    } else {
+#pragma unroll
+        for (int k = 0; k < T / ROWS; ++k)
+#pragma unroll
+            for (int l = 0; l < 4; ++l) tile[y + k * ROWS][x + l] = u[k][l];
     }
     __syncthreads();
-#pragma unroll 4
-    for (int y = threadIdx.x / T; y < T; y += NORM_THREADS / T) {
-        const int i = i0 + y, j = j0 + x;
-        if (i < mat.m && j < mat.ldx) {
-            __half hi, lo;
-            split(mat.transposed ? tile[x][y] : tile[y][x], hi, lo);
-            const size_t at = (size_t)i * mat.ldx + j;
-            reinterpret_cast<__half *>(mat.xhi[0])[at] = hi;
-            reinterpret_cast<__half *>(mat.xlo[0])[at] = lo;
+#pragma unroll
+    for (int k = 0; k < T / ROWS; ++k) {
+        const int i = y + k * ROWS;
+        if (i0 + i < mat.m) {  // (j < ldx, a multiple of the tile's side)
+            const size_t at = (size_t)(i0 + i) * mat.ldx + j0 + x;
+            float w[4];
+#pragma unroll
+            for (int l = 0; l < 4; ++l) w[l] = tile[i][x + l];
+            *reinterpret_cast<uint2 *>(mat.xhi[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
+            if (mat.precise) {
+#pragma unroll
+                for (int l = 0; l < 4; ++l) w[l] -= __half2float(__float2half_rn(w[l]));
+                *reinterpret_cast<uint2 *>(mat.xlo[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
+            }
+        }
+        // block k of the tile's four, a warp for each of its groups of four columns
+        const int lane = threadIdx.x & 31, quad = threadIdx.x >> 5, bi = k >> 1, bj = k & 1;
+        if (i0 + 32 * bi < mat.m) {
+            const float *from = &tile[32 * bi + lane][32 * bj + 4 * quad];
+            float *to = mat.x32 + ((size_t)(i0 / 32 + bi) * (mat.ldx / 32) + j0 / 32 + bj) * 1024 + quad * 128 + lane * 4;
+            *reinterpret_cast<float4 *>(to) = make_float4(from[0], from[1], from[2], from[3]);
         }
     }
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------------
 
-constexpr int EPI_WARPS = 8;
+constexpr int EPI_WARPS = MUON_EPI_WARPS;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;  // producer warp, MMA warp, epilogue
 constexpr int OPERAND = 16384;                // 128 rows (K-major) or 64 x 128 (MN-major) fp16 elements of one step of K = 64
 constexpr int STAGE = 2 * OPERAND;
 constexpr int STAGES = 6;
 constexpr int TMEM_COLS = 512;
-constexpr int SMEM = STAGES * STAGE + 1024;
+constexpr int SMEM = STAGES * STAGE + EPI_WARPS * 4096 + 1024;
 
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -229,9 +298,10 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
     else
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// A box of 64 x 64 elements; a pair's loads are counted by the barrier of its first CTA.
+// One operand of a step: 128 rows of 64 elements (K-major), or, column by column, two blocks of 64 rows of K (MN-major).  A pair's loads are
+// counted by the barrier of its first CTA.
 template <int CG>
-__device__ __forceinline__ void load_box(uint32_t dst, const void *map, int x, int y, uint32_t bar)
+__device__ __forceinline__ void load_rows(uint32_t dst, const void *map, int x, int y, uint32_t bar)
 {
     if constexpr (CG == 1)
         tma_load_2d(dst, map, x, y, bar);
@@ -240,14 +310,29 @@ __device__ __forceinline__ void load_box(uint32_t dst, const void *map, int x, i
                      "r"(x), "r"(y), "r"(bar)
                      : "memory");
 }
-__device__ __forceinline__ void arrive_at(uint32_t bar, bool remote)
+template <int CG>
+__device__ __forceinline__ void load_columns(uint32_t dst, const void *map, int x, int y, uint32_t bar)
 {
-    if (remote)
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(0),
+                     "r"(y), "r"(x / 64), "r"(bar)
+                     : "memory");
     else
-        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
+                     "r"(0), "r"(y), "r"(x / 64), "r"(bar)
+                     : "memory");
 }
-// as mbar_wait_bounded, seeing what another CTA of the cluster did before its arrival
+// (release at the scope of the CTA even where the barrier is another CTA's: one of the cluster's would wait for this warp's stores to memory)
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void arrive_release_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+constexpr long long TASK_WAIT_CYCLES = 20000000000LL;  // ~10 s: what is waited for may be other workers' tasks, long ones for large matrices
+
+__device__ __forceinline__ bool wait_local(uint32_t bar, unsigned parity) { return mbar_wait_bounded(bar, parity, TASK_WAIT_CYCLES); }
+// as wait_local, seeing what another CTA of the cluster did before its arrival
 __device__ __forceinline__ bool wait_cluster(uint32_t bar, unsigned parity)
 {
     const long long t0 = clock64();
@@ -259,184 +344,282 @@ __device__ __forceinline__ bool wait_cluster(uint32_t bar, unsigned parity)
             : "r"(bar), "r"(parity)
             : "memory");
         if (ok) return true;
-        if (clock64() - t0 > WAIT_LIMIT_CYCLES) return false;
+        if (clock64() - t0 > TASK_WAIT_CYCLES) return false;
     }
 }
 
-__device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
-__device__ __forceinline__ uint32_t pack2(float x, float y)
-{
-    const __half2 h = __floats2half2_rn(x, y);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-// 32 consecutive fp16 values of a row (its start a multiple of 64 bytes) to and from fp32.
-__device__ __forceinline__ void load_row32(const uint16_t *p, float (&v)[32])
+// A warp's block of 32 x 32 accumulators on its way through shared memory, from a row a lane, as tensor memory gives it, to pieces of eight
+// columns, as memory wants it: four lanes then cover 32 columns of a row.  16-byte quads are stored where neither the rows' writes, nor the
+// pieces' reads, nor reads down the columns meet in a bank.
+__device__ __forceinline__ int quad_at(int row, int quad) { return row * 32 + ((quad ^ (row & 7) ^ ((row >> 3) << 1)) << 2); }
+__device__ __forceinline__ void stage_rows(float *st, const float (&v)[32], int lane)
 {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const uint4 w = reinterpret_cast<const uint4 *>(p)[q];
-        const float2 a = unpack2(w.x), b = unpack2(w.y), c = unpack2(w.z), d = unpack2(w.w);
-        v[8 * q] = a.x, v[8 * q + 1] = a.y, v[8 * q + 2] = b.x, v[8 * q + 3] = b.y;
-        v[8 * q + 4] = c.x, v[8 * q + 5] = c.y, v[8 * q + 6] = d.x, v[8 * q + 7] = d.y;
-    }
+    for (int k = 0; k < 8; ++k) *reinterpret_cast<float4 *>(st + quad_at(lane, k)) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
 }
-__device__ __forceinline__ void store_row32(uint16_t *p, const float (&v)[32])
+__device__ __forceinline__ void read_piece(const float *st, int row, int q, float (&v)[8])
+{
+    const float4 a = *reinterpret_cast<const float4 *>(st + quad_at(row, 2 * q)), b = *reinterpret_cast<const float4 *>(st + quad_at(row, 2 * q + 1));
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+// rows 8 q .. 8 q + 7 of one column
+__device__ __forceinline__ void read_column(const float *st, int col, int q, float (&v)[8])
 {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        reinterpret_cast<uint4 *>(p)[q] = make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]), pack2(v[8 * q + 4], v[8 * q + 5]),
-                                                     pack2(v[8 * q + 6], v[8 * q + 7]));
-}
-__device__ __forceinline__ void keep_rest(float (&v)[32])  // v - fp16(v)
-{
-#pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
+    for (int k = 0; k < 8; ++k) v[k] = st[quad_at(8 * q + k, col >> 2) + (col & 3)];
 }
 
-// A row piece (row i, columns j0 .. j0 + 31) of a symmetric result, into its place and, off the diagonal tiles, mirrored: there a warp's
-// 32 rows are 32 neighbouring columns.
-__device__ __forceinline__ void store_symmetric(const MuonMat &mat, uint16_t *hi, uint16_t *lo, float (&v)[32], int i, int j0, bool mirror)
+// Eight neighbouring results (of a tensor row, from column c on) to the caller's tensor.
+__device__ __forceinline__ void deliver(const MuonArgs &a, void *out, size_t at, int c, int cols, const float (&o)[8], float keep)
 {
-    const size_t at = (size_t)i * mat.lde + j0;
-    if (mirror) {
+    const int left = cols - c;
+    if (a.to == MUON_TO_PARAMS) {  // o = -lr s O
+        float *x = static_cast<float *>(out) + at;
+        if ((cols & 3) == 0 && left >= 8) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float4 w = reinterpret_cast<float4 *>(x)[q];
+                w.x = fmaf(w.x, keep, o[4 * q]);
+                w.y = fmaf(w.y, keep, o[4 * q + 1]);
+                w.z = fmaf(w.z, keep, o[4 * q + 2]);
+                w.w = fmaf(w.w, keep, o[4 * q + 3]);
+                reinterpret_cast<float4 *>(x)[q] = w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < left) x[k] = fmaf(x[k], keep, o[k]);
+        }
+    } else if (a.out_bf16) {
+        __nv_bfloat16 *p = static_cast<__nv_bfloat16 *>(out) + at;
+        if ((cols & 7) == 0) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(o[2 * q], o[2 * q + 1]);
+                w[q] = *reinterpret_cast<const uint32_t *>(&b);
+            }
+            *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < left) p[k] = __float2bfloat16_rn(o[k]);
+        }
+    } else {
+        float *p = static_cast<float *>(out) + at;
+        if ((cols & 3) == 0 && left >= 8) {
+            reinterpret_cast<float4 *>(p)[0] = make_float4(o[0], o[1], o[2], o[3]);
+            reinterpret_cast<float4 *>(p)[1] = make_float4(o[4], o[5], o[6], o[7]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < left) p[k] = o[k];
+        }
+    }
+}
+
+// ---- epilogues: a warp's block is 32 rows, a lane's row, by 32 columns -------------------------------------------------------------
+
+// The fp16 values of a block on their way out: rows of 64 bytes, the 16-byte pieces of row r at piece ^ (r / 2 % 4), the 64-byte swizzle.
+__device__ __forceinline__ void stage_halves(unsigned char *buf, const uint32_t (&p)[16], int lane)
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<uint4 *>(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
+}
+// Writes a block as fp16 and, where the products need it, what that leaves.  The copies read the buffers after this returns; two alternate.
+// (pad columns and rows: the copy leaves out what lies outside the matrix)
+__device__ __forceinline__ void write_halves(unsigned char *bufs, int &turn, const char *map, const char *map_lo, bool precise, const float (&v)[32], int r0, int j0, int lane)
+{
+    uint32_t p[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) p[k] = pack2(v[2 * k], v[2 * k + 1]);
+    if (lane == 0) {
+        if (precise)
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        else
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    }
+    __syncwarp();
+    unsigned char *buf = bufs + (precise ? 0 : turn * 2048);
+    turn ^= 1;
+    stage_halves(buf, p, lane);
+    if (precise) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const float2 h = unpack2(p[k]);
+            p[k] = pack2(v[2 * k] - h.x, v[2 * k + 1] - h.y);
+        }
+        stage_halves(bufs + 2048, p, lane);
+    }
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+        tma_store_2d(map, j0, r0, smem_u32(buf));
+        if (precise) tma_store_2d(map_lo, j0, r0, smem_u32(bufs + 2048));
+        tma_store_commit();
+    }
+}
+
+// (past the L1, which may hold these addresses as they were an iteration ago)
+__device__ __forceinline__ void load_block(const float *p, float4 (&x)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(p + k * 128));
+}
+__device__ __forceinline__ void store_block(float *p, const float (&v)[32])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) __stcg(reinterpret_cast<float4 *>(p + k * 128), make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
+}
+__device__ __forceinline__ const float &part(const float4 (&x)[8], int k) { return reinterpret_cast<const float *>(x)[k]; }
+
+struct BlockAt {
+    float *master;  // the lane's place in the block
+    uint32_t tmem;
+    int r0, j0, lane;
+    float *st;      // the warp's 4 KB of shared memory
+};
+
+// E = A off the diagonal, d on it.
+__device__ __forceinline__ void block_gram(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn)
+{
+    float v[32];
+    tmem_ld32(b.tmem, v);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] *= t.scale;
+    if (b.r0 == b.j0) {
+        float d = 0.f;
 #pragma unroll
         for (int k = 0; k < 32; ++k)
-            if (j0 + k < mat.m) {
-                __half h, l;
-                split(v[k], h, l);
-                const size_t to = (size_t)(j0 + k) * mat.lde + i;
-                reinterpret_cast<__half *>(hi)[to] = h;
-                if (mat.precise) reinterpret_cast<__half *>(lo)[to] = l;
-            }
-    }
-    store_row32(hi + at, v);
-    if (mat.precise) {
-        keep_rest(v);
-        store_row32(lo + at, v);
-    }
-}
-
-template <int PHASE>
-__device__ __forceinline__ void epilogue(const MuonArgs &a, const MuonMat &mat, float (&v)[32], int i, int j0, bool mirror, int parity)
-{
-    if (i >= mat.m) return;
-    if constexpr (PHASE == MUON_GRAM) {
-        if (j0 >= mat.m) return;
-        const float s = mat.inv_S * mat.inv_S * MUON_EF_SCALE;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            v[k] *= s;
-            if (j0 + k == i) {
-                mat.d[i] = v[k] * MUON_EF_INV;
+            if (k == b.lane) {
+                d = v[k];
                 v[k] = 0.f;
             }
-        }
-        store_symmetric(mat, mat.ehi, mat.elo, v, i, j0, mirror);
-    } else if constexpr (PHASE == MUON_POLY) {
-        if (j0 >= mat.m) return;
-        const size_t at = (size_t)i * mat.lde + j0;
-        float e[32];
-        load_row32(mat.ehi + at, e);
-        if (mat.precise) {
-            float l[32];
-            load_row32(mat.elo + at, l);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) e[k] += l[k];
-        }
-        const float di = mat.d[i], base = fmaf(a.c, di, a.b);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            const float dj = j0 + k < mat.m ? mat.d[j0 + k] : 0.f;
-            const float f = fmaf(fmaf(a.c, dj, base), e[k], a.c * MUON_EF_INV * v[k]);
-            if (j0 + k == i) mat.beta[i] = fmaf(a.b, di, a.c * fmaf(di, di, v[k] * (MUON_EF_INV * MUON_EF_INV)));
-            v[k] = j0 + k == i ? 0.f : f;
-        }
-        store_symmetric(mat, mat.fhi, mat.flo, v, i, j0, mirror);
-    } else {
-        if (j0 >= mat.n) return;
-        const size_t at = (size_t)i * mat.ldx + j0;
-        const float lin = a.a + mat.beta[i];
-        {
-            float x[32];
-            load_row32(mat.xlo[parity] + at, x);
-            float h[32];
-            load_row32(mat.xhi[parity] + at, h);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = fmaf(lin, h[k] + x[k], v[k] * MUON_EF_INV);
-        }
-        if constexpr (PHASE == MUON_UPDATE) {
-            store_row32(mat.xhi[parity ^ 1] + at, v);
-            keep_rest(v);
-            store_row32(mat.xlo[parity ^ 1] + at, v);
-        } else {
-            const bool params = a.to == MUON_TO_PARAMS;
-            const float keep = 1.f - a.lr * a.wd, scale = params ? -a.lr * mat.step_scale * mat.inv_S : mat.inv_S;
-            const int cols = mat.transposed ? mat.m : mat.n;
-            const size_t to = mat.transposed ? (size_t)j0 * cols + i : (size_t)i * cols + j0;
-            const int step = mat.transposed ? cols : 1;
-            void *out = a.out[mat.tensor];
-            const bool whole = !mat.transposed && cols % 8 == 0 && j0 + 32 <= cols;
-            if (params) {
-                float *x = static_cast<float *>(out) + to;
-                if (whole) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        float4 w = reinterpret_cast<float4 *>(x)[q];
-                        w.x = fmaf(w.x, keep, v[4 * q] * scale);
-                        w.y = fmaf(w.y, keep, v[4 * q + 1] * scale);
-                        w.z = fmaf(w.z, keep, v[4 * q + 2] * scale);
-                        w.w = fmaf(w.w, keep, v[4 * q + 3] * scale);
-                        reinterpret_cast<float4 *>(x)[q] = w;
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (j0 + k < mat.n) x[(size_t)k * step] = fmaf(x[(size_t)k * step], keep, v[k] * scale);
-                }
-            } else if (a.out_bf16) {
-                __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out) + to;
-                if (whole) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            const __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * q + 2 * p] * scale, v[8 * q + 2 * p + 1] * scale);
-                            w[p] = *reinterpret_cast<const uint32_t *>(&b);
-                        }
-                        reinterpret_cast<uint4 *>(o)[q] = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (j0 + k < mat.n) o[(size_t)k * step] = __float2bfloat16_rn(v[k] * scale);
-                }
-            } else {
-                float *o = static_cast<float *>(out) + to;
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (j0 + k < mat.n) o[(size_t)k * step] = v[k] * scale;
-            }
-        }
+        __stcg(t.vec + b.r0 + b.lane, d * MUON_EF_INV);
     }
+    store_block(b.master, v);
+    write_halves(reinterpret_cast<unsigned char *>(b.st), turn, a.maps + (size_t)t.out * MUON_MAP_BYTES, a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, t.parts > 1, v, b.r0, b.j0,
+                 b.lane);
 }
 
-// Persistent CTAs (CG = 2: pairs) over the tiles.  One warp loads, one issues the MMAs, eight read accumulators back: two of them, so that
-// the products of a tile run beside the epilogue of the one before.
-template <int PHASE, int CG>
-__global__ void __launch_bounds__(THREADS, 1) muon_product_kernel(MuonArgs a, const MuonTile *tiles, int n_tiles, int parity)
+// F = (b + c (d_i + d_j)) E + c E^2 off the diagonal, beta = b d + c (d^2 + E^2) on it.
+__device__ __forceinline__ void block_poly(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&e)[8], float di)
+{
+    float v[32];
+    float4 dj[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dj[k] = __ldcg(reinterpret_cast<const float4 *>(t.vec + b.j0) + k);
+    tmem_ld32(b.tmem, v);
+    if (b.r0 == b.j0) {
+        float square = 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            if (k == b.lane) square = v[k];
+        __stcg(t.beta + b.r0 + b.lane, fmaf(a.b, di, a.c * fmaf(di, di, square * (MUON_EF_INV * MUON_EF_INV))));
+    }
+    const float base = fmaf(a.c, di, a.b), scale = a.c * MUON_EF_INV;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(fmaf(a.c, part(dj, k), base), part(e, k), scale * v[k]);
+    if (b.r0 == b.j0) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            if (k == b.lane) v[k] = 0.f;
+    }
+    write_halves(reinterpret_cast<unsigned char *>(b.st), turn, a.maps + (size_t)t.out * MUON_MAP_BYTES, a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, t.parts > 1, v, b.r0, b.j0,
+                 b.lane);
+}
+
+// X <- (a + beta) X + F X
+__device__ __forceinline__ void block_update(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&x)[8], float lin)
+{
+    float v[32];
+    tmem_ld32(b.tmem, v);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(lin, part(x, k), v[k] * MUON_EF_INV);
+    store_block(b.master, v);
+    write_halves(reinterpret_cast<unsigned char *>(b.st), turn, a.maps + (size_t)t.out * MUON_MAP_BYTES, a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, t.parts > 1, v, b.r0, b.j0,
+                 b.lane);
+}
+
+// The same, the last time: to the caller's tensor.
+__device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, const float4 (&x)[8], float lin)
+{
+    const bool params = a.to == MUON_TO_PARAMS;
+    const float scale = params ? -a.lr * t.step_scale : t.scale, keep = 1.f - a.lr * a.wd;
+    void *out = a.out[t.tensor];
+    {
+        float v[32];
+        tmem_ld32(b.tmem, v);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = fmaf(lin, part(x, k), v[k] * MUON_EF_INV) * scale;
+        stage_rows(b.st, v, b.lane);
+    }
+    __syncwarp();
+    const int sub = b.lane >> 2, q = b.lane & 3;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+        if (t.transposed) {  // row j of the tensor is column j of X
+            const int r = b.j0 + 8 * i + sub, c = b.r0 + 8 * q;
+            read_column(b.st, 8 * i + sub, q, v);
+            if (r < t.width && c < t.m) deliver(a, out, (size_t)r * t.m + c, c, t.m, v, keep);
+        } else {
+            const int r = b.r0 + 8 * i + sub, c = b.j0 + 8 * q;
+            read_piece(b.st, 8 * i + sub, q, v);
+            if (r < t.m && c < t.width) deliver(a, out, (size_t)r * t.width + c, c, t.width, v, keep);
+        }
+    }
+    __syncwarp();
+}
+
+__device__ __forceinline__ unsigned load_acquire(const unsigned *p)
+{
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+// Until `need` completions of a matrix are there.  False when that takes too long or another CTA has given up.
+__device__ __forceinline__ bool wait_task(const unsigned *done, unsigned need, const int *status)
+{
+    if (load_acquire(done) >= need) return true;
+    const long long t0 = clock64();
+    for (unsigned n = 0; load_acquire(done) < need; ++n) {
+        __nanosleep(20);
+        if ((n & 1023) == 1023 && (clock64() - t0 > TASK_WAIT_CYCLES || *static_cast<const volatile int *>(status) != 0)) return false;
+    }
+    return true;
+}
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+struct alignas(16) RingEntry {
+    MuonProduct p;
+    int i, j, end, pad;
+};
+
+// All products of all iterations, by persistent workers (CTAs; CG = 2: pairs).  Tasks are drawn in the list's order from one counter, so
+// whatever a task waits for is done already or in the hands of a worker that runs: no worker has to be resident for another to go on.
+// One warp loads, one issues the MMAs, eight read accumulators back: two of them, so that the products of a task run beside the epilogue
+// of the one before.  The loading lane of a worker's first CTA draws the tasks and waits until they may start; those of both CTAs put
+// what the other warps need to know of one into a ring.
+// E and F are symmetric and exist above the diagonal only: left of it a panel's operand is loaded from the rows above, as its transpose.
+template <int CG>
+__global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
 {
     const StreamOrder order(1);
     constexpr int TILE = 128 * CG;  // of both sides
-    constexpr bool B_MN = PHASE >= MUON_UPDATE;  // X as K x N: its rows run along K
-    constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)B_MN << 16) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+    constexpr int RING = 4;
     extern __shared__ unsigned char raw[];
-    __shared__ unsigned long long bars[2 * STAGES + 4 + 1];
+    __shared__ unsigned long long bars[2 * STAGES + 4 + 4 * RING + 1];
+    __shared__ RingEntry ring[RING];
+    __shared__ int drawn_ring[RING];
     __shared__ uint32_t tmem_slot;
     const uint32_t raw_s = smem_u32(raw), base = (raw_s + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, t_full = empty + 8 * STAGES, t_empty = t_full + 16, drained = t_empty + 16;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, t_full = empty + 8 * STAGES, t_empty = t_full + 16, r_full = t_empty + 16,
+                   r_empty = r_full + 8 * RING, q_full = r_empty + 8 * RING, q_empty = q_full + 8 * RING, drained = q_empty + 8 * RING;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -445,6 +628,12 @@ __global__ void __launch_bounds__(THREADS, 1) muon_product_kernel(MuonArgs a, co
         for (int s = 0; s < 2; ++s) {
             mbar_init(t_full + 8 * s, 1);
             mbar_init(t_empty + 8 * s, CG * EPI_WARPS);
+        }
+        for (int s = 0; s < RING; ++s) {
+            mbar_init(r_full + 8 * s, 1);
+            mbar_init(r_empty + 8 * s, EPI_WARPS + (rank == 0 ? 1 : 0));  // the epilogues and the MMA warp
+            mbar_init(q_full + 8 * s, 1);
+            mbar_init(q_empty + 8 * s, 1);
         }
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -465,60 +654,114 @@ __global__ void __launch_bounds__(THREADS, 1) muon_product_kernel(MuonArgs a, co
     if (CG == 2) cluster_sync();
     tc_after();
     const uint32_t tmem = tmem_slot;
-    const int stride = gridDim.x / CG, start = blockIdx.x / CG;
     bool ok = true;
+    int slot = 0;  // of the ring
+    unsigned turn = 0;
+    auto next_slot = [&] {
+        if (++slot == RING) slot = 0, turn ^= 1;
+    };
 
     if (warp == 0) {
         if (lane == 0) {
             const uint32_t full0 = CG == 2 ? map_to_rank(full, 0) : full;
-            int stage = 0, last_mat = -1;
+            int stage = 0, last_product = -1;
             unsigned phase = 0, used = 0;
-            for (int t = start; ok && t < n_tiles; t += stride) {
-                const MuonTile tl = tiles[t];
-                const MuonMat &mat = a.mats[tl.mat];
-                const char *maps = a.maps + (size_t)mat.maps * MUON_MAP_BYTES;
-                // left operand (and its lo part), right operand
-                const int left = PHASE == MUON_GRAM ? MUON_MAP_X0 + parity : PHASE == MUON_POLY ? MUON_MAP_E : MUON_MAP_F;
-                const int right = PHASE == MUON_POLY ? MUON_MAP_E : MUON_MAP_X0 + parity;
-                const int left_lo = PHASE == MUON_GRAM ? MUON_MAP_XLO0 + parity : left + 1;
-                const int right_lo = PHASE == MUON_POLY ? MUON_MAP_ELO : MUON_MAP_XLO0 + parity;
-                if (tl.mat != last_mat) {
-                    tmap_acquire(maps + left * MUON_MAP_BYTES);
-                    tmap_acquire(maps + right * MUON_MAP_BYTES);
-                    if (mat.precise) {
-                        tmap_acquire(maps + left_lo * MUON_MAP_BYTES);
-                        tmap_acquire(maps + right_lo * MUON_MAP_BYTES);
-                    }
-                    last_mat = tl.mat;
+            unsigned drawn = rank == 0 ? atomicAdd(a.next_task, 1u) : 0u;
+            for (;;) {
+                int t;
+                if (rank == 0) {
+                    t = drawn < (unsigned)n_tasks ? (int)drawn : -1;
+                    if (t >= 0) drawn = atomicAdd(a.next_task, 1u);  // (needed when this task's loads are under way)
+                } else {
+                    ok = wait_cluster(q_full + 8 * slot, turn);
+                    if (!ok) break;
+                    t = *static_cast<volatile int *>(drawn_ring + slot);
+                    arrive_cluster(map_to_rank(q_empty + 8 * slot, 0));
                 }
-                const int K = PHASE == MUON_GRAM ? mat.n : mat.m, steps = (K + 63) / 64, parts = mat.precise ? 3 : 1;
-                const int row = tl.i * TILE + (int)rank * 128, col = tl.j * TILE + (int)rank * 128;
-                for (int part = 0; ok && part < parts; ++part) {  // hi hi, hi lo, lo hi
-                    const char *ml = maps + (part == 2 ? left_lo : left) * MUON_MAP_BYTES, *mr = maps + (part == 1 ? right_lo : right) * MUON_MAP_BYTES;
-                    for (int k = 0; k < steps; ++k) {
-                        ok = CG == 2 ? wait_cluster(empty + 8 * stage, phase ^ 1) : mbar_wait_bounded(empty + 8 * stage, phase ^ 1);
+                MuonTask tk{0, 0, 0};
+                if (t >= 0) tk = tasks[t];
+                uint4 words[6];
+                {
+                    const uint4 *from = reinterpret_cast<const uint4 *>(products + tk.product);
+#pragma unroll
+                    for (int k = 0; k < 6; ++k) words[k] = __ldg(from + k);
+                }
+                const MuonProduct &p = *reinterpret_cast<const MuonProduct *>(words);
+                const char *left = a.maps + (size_t)p.left * MUON_MAP_BYTES, *right = a.maps + (size_t)p.right * MUON_MAP_BYTES;
+                const char *left_lo = a.maps + (size_t)p.left_lo * MUON_MAP_BYTES, *right_lo = a.maps + (size_t)p.right_lo * MUON_MAP_BYTES;
+                if (t >= 0 && tk.product != last_product) {
+                    last_product = tk.product;
+                    for (int lo = 0; lo < (p.parts > 1 ? 2 : 1); ++lo) {
+                        const char *l = lo ? left_lo : left, *r = lo ? right_lo : right;
+                        tmap_acquire(l);
+                        tmap_acquire(r);
+                        if (p.phase != MUON_GRAM) {
+                            tmap_acquire(l + MUON_MAP_MN * MUON_MAP_BYTES);
+                            tmap_acquire(r + MUON_MAP_MN * MUON_MAP_BYTES);
+                        }
+                        if (p.phase != MUON_FINAL) tmap_acquire(a.maps + (size_t)(lo ? p.out_lo : p.out) * MUON_MAP_BYTES);
+                    }
+                }
+                if (rank == 0 && t >= 0 && !wait_task(a.done + p.mat, p.need, a.status)) {
+                    ok = false;
+                    break;
+                }
+                if (CG == 2 && rank == 0) {
+                    ok = wait_cluster(q_empty + 8 * slot, turn ^ 1);
+                    if (!ok) break;
+                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(drawn_ring + slot), 1)), "r"(t) : "memory");
+                    arrive_release_cluster(map_to_rank(q_full + 8 * slot, 1));
+                }
+                ok = wait_local(r_empty + 8 * slot, turn ^ 1);
+                if (!ok) break;
+                {
+                    uint4 *to = reinterpret_cast<uint4 *>(ring + slot);
+#pragma unroll
+                    for (int k = 0; k < 6; ++k) to[k] = words[k];
+                    to[6] = make_uint4((unsigned)(int)tk.i, (unsigned)(int)tk.j, t < 0 ? 1u : 0u, 0u);
+                }
+                arrive(r_full + 8 * slot);
+                next_slot();
+                if (t < 0) break;
+                fence_proxy_async_all();
+                const int row = tk.i * TILE + (int)rank * 128, col = tk.j * TILE + (int)rank * 128;
+                const int left_rows = p.phase == MUON_GRAM ? 0 : tk.i * TILE;  // from here on K's elements lie in the panel's rows
+                const int right_rows = p.phase == MUON_GRAM ? 0 : p.phase == MUON_POLY ? tk.j * TILE : 1 << 30;
+                if (p.phase >= MUON_POLY) {  // the epilogue reads the tile of x32 or e32
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int b = p.blocks - tk.j * (TILE / 32);
+                        const unsigned bytes = (unsigned)(b < TILE / 32 ? b : TILE / 32) * 4096u;
+                        const float *at = p.master + ((size_t)(row / 32 + k) * p.blocks + tk.j * (TILE / 32)) * 1024;
+                        if (row + 32 * k < p.m) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
+                    }
+                }
+                for (int part = 0; ok && part < p.parts; ++part) {  // hi hi, hi lo, lo hi
+                    const char *ml = part == 2 ? left_lo : left, *mr = part == 1 ? right_lo : right;
+                    for (int k = 0; k < p.steps; ++k) {
+                        ok = wait_local(empty + 8 * stage, phase ^ 1);
                         if (!ok) break;
                         const uint32_t bar = full0 + 8 * stage, A = base + stage * STAGE, B = A + OPERAND;
                         if (rank == 0) mbar_expect_tx(full + 8 * stage, CG * STAGE);
-                        load_box<CG>(A, ml, 64 * k, row, bar);
-                        load_box<CG>(A + OPERAND / 2, ml, 64 * k, row + 64, bar);
-                        if (B_MN) {
-                            load_box<CG>(B, mr, col, 64 * k, bar);
-                            load_box<CG>(B + OPERAND / 2, mr, col + 64, 64 * k, bar);
-                        } else {
-                            load_box<CG>(B, mr, 64 * k, col, bar);
-                            load_box<CG>(B + OPERAND / 2, mr, 64 * k, col + 64, bar);
-                        }
+                        if (64 * k >= left_rows)
+                            load_rows<CG>(A, ml, 64 * k, row, bar);
+                        else
+                            load_columns<CG>(A, ml + MUON_MAP_MN * MUON_MAP_BYTES, row, 64 * k, bar);
+                        if (64 * k >= right_rows)
+                            load_rows<CG>(B, mr, 64 * k, col, bar);
+                        else
+                            load_columns<CG>(B, mr + MUON_MAP_MN * MUON_MAP_BYTES, col, 64 * k, bar);
                         ++used;
                         if (++stage == STAGES) stage = 0, phase ^= 1;
                     }
                 }
+                if (!ok) break;
             }
             // before the CTA ends, every stage has been read (after a failure: waited for, as long as a wait lasts)
             for (int s = 0; s < STAGES && used; ++s) {
                 if (used >= (unsigned)STAGES || s < stage) {
                     const unsigned last = s < stage ? phase : phase ^ 1;
-                    if (!(CG == 2 ? wait_cluster(empty + 8 * s, last) : mbar_wait_bounded(empty + 8 * s, last))) ok = false;
+                    if (!wait_local(empty + 8 * s, last)) ok = false;
                 }
             }
         }
@@ -526,31 +769,44 @@ __global__ void __launch_bounds__(THREADS, 1) muon_product_kernel(MuonArgs a, co
         if (lane == 0 && rank == 0) {
             int stage = 0, n_done = 0;
             unsigned phase = 0;
-            for (int t = start; ok && t < n_tiles; t += stride, ++n_done) {
-                const MuonMat &mat = a.mats[tiles[t].mat];
-                const int K = PHASE == MUON_GRAM ? mat.n : mat.m, steps = (K + 63) / 64 * (mat.precise ? 3 : 1);
+            for (;; ++n_done) {
+                ok = wait_local(r_full + 8 * slot, turn);
+                if (!ok) break;
+                const RingEntry &e = ring[slot];
+                const int end = e.end, kind = e.p.phase, steps = e.p.steps, parts = e.p.parts;
+                const int left_rows = kind == MUON_GRAM ? 0 : e.i * TILE, right_rows = kind == MUON_GRAM ? 0 : kind == MUON_POLY ? e.j * TILE : 1 << 30;
+                arrive(r_empty + 8 * slot);
+                next_slot();
+                if (end) break;
                 const int acc = n_done & 1;
-                ok = CG == 2 ? wait_cluster(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1) : mbar_wait_bounded(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1);
+                ok = CG == 2 ? wait_cluster(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1) : wait_local(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1);
                 if (!ok) break;
                 tc_after();
                 const uint32_t d = tmem + acc * 256;
-                for (int k = 0; k < steps; ++k) {
-                    ok = CG == 2 ? wait_cluster(full + 8 * stage, phase) : mbar_wait_bounded(full + 8 * stage, phase);
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t A = base + stage * STAGE;
-                    // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row.  MN-major: blocks of 64 columns
-                    // 8192 bytes apart, groups of 8 rows of K 1024.
-                    uint64_t da = operand_desc(A, 16, 1024), db = operand_desc(A + OPERAND, B_MN ? 8192 : 16, 1024);
+                uint32_t accumulate = 0;
+                for (int part = 0; ok && part < parts; ++part)
+                    for (int k = 0; k < steps; ++k) {
+                        // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row.  MN-major: blocks of 64
+                        // columns 8192 bytes apart, groups of 8 rows of K 1024.
+                        const bool a_mn = 64 * k < left_rows, b_mn = 64 * k < right_rows;
+                        const uint32_t idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+                        const uint32_t A = base + stage * STAGE;
+                        uint64_t da = operand_desc(A, a_mn ? 8192 : 16, 1024), db = operand_desc(A + OPERAND, b_mn ? 8192 : 16, 1024);
+                        const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
+                        ok = wait_local(full + 8 * stage, phase);
+                        if (!ok) break;
+                        tc_after();
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        mma_f16<CG>(d, da, db, IDESC, (k | kk) != 0);
-                        da += 32 >> 4;
-                        db += (B_MN ? 2048 : 32) >> 4;
+                        for (int kk = 0; kk < 4; ++kk) {
+                            mma_f16<CG>(d, da, db, idesc, accumulate);
+                            accumulate = 1;
+                            da += a_step;
+                            db += b_step;
+                        }
+                        mma_commit<CG>(empty + 8 * stage);
+                        if (++stage == STAGES) stage = 0, phase ^= 1;
                     }
-                    mma_commit<CG>(empty + 8 * stage);
-                    if (++stage == STAGES) stage = 0, phase ^= 1;
-                }
+                if (!ok) break;
                 mma_commit<CG>(t_full + 8 * acc);
             }
             if (!ok) {  // what was issued ends before the tensor memory is freed
@@ -564,33 +820,69 @@ __global__ void __launch_bounds__(THREADS, 1) muon_product_kernel(MuonArgs a, co
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;  // a warp reads the lanes 32 (warp % 4) .. + 31; the two of a quarter share its columns
         const uint32_t t_empty0 = CG == 2 ? map_to_rank(t_empty, 0) : t_empty;
-        int n_done = 0;
-        for (int t = start; t < n_tiles; t += stride, ++n_done) {
-            const MuonTile tl = tiles[t];
-            const MuonMat &mat = a.mats[tl.mat];
+        float *st = reinterpret_cast<float *>(raw + (base - raw_s) + STAGES * STAGE) + (warp - 2) * 1024;
+        int out_turn = 0;
+        for (int n_done = 0;; ++n_done) {
+            ok = wait_local(r_full + 8 * slot, turn);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const MuonProduct t = ring[slot].p;
+            const int ti = ring[slot].i, tj = ring[slot].j, end = ring[slot].end;
+            __syncwarp();
+            if (lane == 0) arrive(r_empty + 8 * slot);
+            next_slot();
+            if (end) break;
+            const int r0 = ti * TILE + (int)rank * 128 + q * 32, first = tj * TILE + half * (TILE / 2);
+            const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 31) / 32, TILE / 64) : 0;
             const int acc = n_done & 1;
-            ok = CG == 2 ? wait_cluster(t_full + 8 * acc, (n_done >> 1) & 1) : mbar_wait_bounded(t_full + 8 * acc, (n_done >> 1) & 1);
+            float *master = t.master + ((size_t)(r0 / 32) * t.blocks + first / 32) * 1024 + lane * 4;
+            float4 x[8], next[8];
+            float row = 0.f;
+            if (blocks > 0 && t.phase != MUON_GRAM) {
+                load_block(master, next);
+                row = __ldcg(t.vec + r0 + lane);
+                if (t.phase != MUON_POLY) row += a.a;
+            }
+            ok = wait_local(t_full + 8 * acc, (n_done >> 1) & 1);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_after();
-            const int i = tl.i * TILE + (int)rank * 128 + q * 32 + lane;
-            const bool mirror = PHASE <= MUON_POLY && tl.i != tl.j;
+            auto each_block = [&](auto use) {
 #pragma unroll 1
-            for (int c = half * (TILE / 2); c < (half + 1) * (TILE / 2); c += 32) {
-                float v[32];
-                tmem_ld32(tmem + acc * 256 + c + ((uint32_t)(q * 32) << 16), v);
-                epilogue<PHASE>(a, mat, v, i, tl.j * TILE + c, mirror, parity);
-                __syncwarp();
-            }
+                for (int b = 0; b < blocks; ++b) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = next[k];
+                    if (t.phase != MUON_GRAM && b + 1 < blocks) load_block(master + (b + 1) * 1024, next);
+                    use(BlockAt{master + b * 1024, tmem + acc * 256 + half * (TILE / 2) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, st});
+                }
+            };
+            if (t.phase == MUON_GRAM)
+                each_block([&](const BlockAt &b) { block_gram(a, t, b, out_turn); });
+            else if (t.phase == MUON_POLY)
+                each_block([&](const BlockAt &b) { block_poly(a, t, b, out_turn, x, row); });
+            else if (t.phase == MUON_UPDATE)
+                each_block([&](const BlockAt &b) { block_update(a, t, b, out_turn, x, row); });
+            else
+                each_block([&](const BlockAt &b) { block_final(a, t, b, x, row); });
             tc_before();
             __syncwarp();
-            if (lane == 0) arrive_at(t_empty0 + 8 * acc, CG == 2);
+            if (lane == 0) {
+                if (CG == 2)
+                    arrive_cluster(t_empty0 + 8 * acc);
+                else
+                    arrive(t_empty0 + 8 * acc);
+                if (t.phase != MUON_FINAL) {
+                    // the copies are written; with them and this warp's other stores the completion is told
+                    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                    fence_proxy_async_all();
+                    asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.done + t.mat), "r"(1u) : "memory");
+                }
+            }
+            __syncwarp();
         }
     }
     if (!ok) atomicExch(a.status, DEMO_DEV_TIMEOUT);
     __syncwarp();
-    // the next launch's copies read through the asynchronous proxy what these warps stored
-    asm volatile("fence.proxy.async;" ::: "memory");
     tc_before();
     __syncthreads();
     if (CG == 2) cluster_sync();
@@ -603,16 +895,16 @@ __global__ void __launch_bounds__(THREADS, 1) muon_product_kernel(MuonArgs a, co
     }
 }
 
-template <int PHASE, int CG>
-cudaError_t launch_product(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int parity, DemoLaunch &dev, cudaStream_t stream)
+template <int CG>
+cudaError_t launch_products(const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, DemoLaunch &dev, cudaStream_t stream)
 {
-    const void *kernel = reinterpret_cast<const void *>(muon_product_kernel<PHASE, CG>);
+    const void *kernel = reinterpret_cast<const void *>(muon_products_kernel<CG>);
     cudaError_t err = demo_allow_smem(dev, kernel);
     if (err != cudaSuccess) return err;
     const int most = dev.sm_count / CG;
-    const int grid = (n_tiles < most ? n_tiles : most) * CG;
+    const int grid = (n_tasks < most ? n_tasks : most) * CG;
     MuonArgs args = a;
-    void *params[] = {&args, &tiles, &n_tiles, &parity};
+    void *params[] = {&args, &products, &tasks, &n_tasks};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -629,17 +921,6 @@ cudaError_t launch_product(const MuonArgs &a, const MuonTile *tiles, int n_tiles
     return cudaLaunchKernelExC(&cfg, kernel, params);
 }
 
-template <int CG>
-cudaError_t launch_phase(int phase, const MuonArgs &a, const MuonTile *tiles, int n_tiles, int parity, DemoLaunch &dev, cudaStream_t stream)
-{
-    switch (phase) {
-        case MUON_GRAM: return launch_product<MUON_GRAM, CG>(a, tiles, n_tiles, parity, dev, stream);
-        case MUON_POLY: return launch_product<MUON_POLY, CG>(a, tiles, n_tiles, parity, dev, stream);
-        case MUON_UPDATE: return launch_product<MUON_UPDATE, CG>(a, tiles, n_tiles, parity, dev, stream);
-        default: return launch_product<MUON_FINAL, CG>(a, tiles, n_tiles, parity, dev, stream);
-    }
-}
-
 }  // namespace
 
 cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n_pieces, DemoLaunch &, cudaStream_t stream)
@@ -649,14 +930,14 @@ cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_norm_kernel), n_pieces, NORM_THREADS, 0, stream, params);
 }
 
-cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, DemoLaunch &, cudaStream_t stream)
+cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, DemoLaunch &, cudaStream_t stream)
 {
     MuonArgs args = a;
-    void *params[] = {&args, &tiles};
+    void *params[] = {&args, &tiles, &first_mat, &n_mats};
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_pack_kernel), n_tiles, NORM_THREADS, 0, stream, params);
 }
 
-cudaError_t muon_launch_product(int phase, bool pair, int parity, const MuonArgs &a, const MuonTile *tiles, int n_tiles, DemoLaunch &dev, cudaStream_t stream)
+cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, DemoLaunch &dev, cudaStream_t stream)
 {
-    return pair ? launch_phase<2>(phase, a, tiles, n_tiles, parity, dev, stream) : launch_phase<1>(phase, a, tiles, n_tiles, parity, dev, stream);
+    return pair ? launch_products<2>(a, products, tasks, n_tasks, dev, stream) : launch_products<1>(a, products, tasks, n_tasks, dev, stream);
 }

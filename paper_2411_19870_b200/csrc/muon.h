@@ -17,12 +17,15 @@ demo_status demo_decode_places(const demo_ctx *ctx, int device, const demo_tenso
 demo_status demo_decode_momentum(demo_ctx *ctx, const void *const *payloads, int32_t n_payloads, float *const *to, float *momentum,
                                  size_t momentum_bytes, cudaStream_t stream);
 
-// One matrix.  The kernels work on X with `m` <= `n`: a tensor with more rows than columns is held transposed.  X lies in the workspace
-// scaled by the power of two `S`, as hi + lo (two fp16 matrices of `ldx` elements a row), twice: an iteration reads one and writes the other.
-// Gram matrix A = D + E: d holds its diagonal, E (fp16, `lde` elements a row) the rest; F and beta are the polynomial of A, split the same way.
+// One matrix.  The kernels work on X with `m` <= `n`: a tensor with more rows than columns is held transposed.  In the workspace, scaled by
+// the power of two `S`:
+//   X     fp16 (twice: an iteration reads one and writes the other; lo parts only for `precise` matrices), rows of `ldx` elements, and x32, fp32
+//   A     its diagonal d; the rest, E = A - D, fp16, rows of `lde` elements, and e32, fp32.  Only tiles on and above the diagonal exist.
+//   F, beta  the polynomial of A, split the same way
+// x32 and e32 lie in blocks of 32 x 32 as the epilogues' lanes hold them: eight groups of four columns, in each 32 rows of four elements.
 struct MuonMat {
     int m, n;
-    int ldx, lde;
+    int ldx, lde;      // multiples of 64
     int transposed;    // 1: X is the tensor's transpose
     int precise;       // 1: products take the lo parts, too
     int tensor;        // position in the caller's pointer arrays
@@ -33,10 +36,13 @@ struct MuonMat {
     float step_scale;  // of the update: x <- x - lr (step_scale O + wd x)
     uint16_t *xhi[2], *xlo[2];
     uint16_t *ehi, *elo, *fhi, *flo;
+    float *x32, *e32;
     float *d, *beta;
 };
-// Tensor maps of a matrix (boxes of 64 x 64 fp16 elements, 128-byte swizzle).
-enum { MUON_MAP_X0 = 0, MUON_MAP_X1 = 1, MUON_MAP_XLO0 = 2, MUON_MAP_XLO1 = 3, MUON_MAP_E = 4, MUON_MAP_ELO = 5, MUON_MAP_F = 6, MUON_MAP_FLO = 7, MUON_MAPS = 8 };
+// Tensor maps of a matrix, three of each of these: boxes of 128 rows x 64 columns (an operand whose rows run along K), two of 64 x 64 side
+// by side (one whose columns do), both with 128-byte swizzle, and 32 x 32 with 64-byte swizzle (what an epilogue writes).
+enum { MUON_MAP_X0 = 0, MUON_MAP_X1 = 1, MUON_MAP_XLO0 = 2, MUON_MAP_XLO1 = 3, MUON_MAP_E = 4, MUON_MAP_ELO = 5, MUON_MAP_F = 6, MUON_MAP_FLO = 7 };
+constexpr int MUON_MAP_MN = 8, MUON_MAP_OUT = 16, MUON_MAPS = 24;
 constexpr int MUON_MAP_BYTES = 128;
 
 // E and F lie in the workspace 256 times as large: entries of 1/m and less, and their lo parts, stay in fp16's normal range (of rank one,
@@ -51,6 +57,30 @@ struct MuonTile {
     short i, j;  // tile row and column
 };
 
+// The products of all matrices are one list of tasks, a tile each; workers draw them in order, so a task may wait for what earlier ones
+// write: `need` completions of its matrix's (each warp of an epilogue is one).
+enum { MUON_GRAM = 0, MUON_POLY = 1, MUON_UPDATE = 2, MUON_FINAL = 3 };
+struct MuonTask {
+    int product;
+    short i, j;
+};
+struct alignas(16) MuonProduct {  // what the tasks of one product of one matrix share
+    int phase, mat;
+    unsigned need;
+    int steps;               // of K = 64
+    int parts;               // 1: hi hi; 3: hi lo and lo hi, too
+    int left, right, out;    // tensor maps of the operands and of the result
+    int left_lo, right_lo, out_lo;
+    int blocks;              // of x32 / e32 in a row of them
+    int m, width;            // of the result
+    int tensor, transposed;
+    float *master;           // e32 (written by GRAM, read by POLY), x32
+    float *vec;              // d (GRAM writes it, POLY reads it), beta
+    float *beta;             // POLY: written
+    float scale, step_scale; // GRAM: of E; FINAL: of O, of the update
+};
+static_assert(sizeof(MuonProduct) == 96, "read as six 16-byte pieces");
+
 // What the update is formed from and what becomes of it.
 enum { MUON_FROM_STEP = 0, MUON_FROM_INPUT = 1 };   // u = g + mu m' (or m'), m' = mu m + g; or u = the input itself
 enum { MUON_TO_PARAMS = 0, MUON_TO_OUTPUT = 1 };
@@ -61,6 +91,10 @@ struct MuonArgs {
     float *const *mom;     // device array (MUON_FROM_STEP)
     void *const *out;      // device array: parameters (fp32) or outputs
     double *partials;      // device: a sum of squares for each piece
+    unsigned *ready;       // device: pieces of each matrix that are summed up, zero between launches
+    float2 *scales;        // device: of each matrix, S / (||u|| + eps) in two factors
+    unsigned *done;        // device: completions of each matrix's tasks
+    unsigned *next_task;   // device
     int from, to;
     int in_bf16, out_bf16;
     int nesterov;
@@ -69,11 +103,10 @@ struct MuonArgs {
     int *status;
 };
 
-enum { MUON_GRAM = 0, MUON_POLY = 1, MUON_UPDATE = 2, MUON_FINAL = 3 };
-
 // Momentum update and the pieces' sums of squares; pieces [0, n_pieces) of the matrices [first, first + n).
 cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n_pieces, DemoLaunch &dev, cudaStream_t stream);
-// X = S u / (||u|| + eps), as hi + lo.
-cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, DemoLaunch &dev, cudaStream_t stream);
-// One product of every listed tile.  pair: tiles of 256 x 256 by clusters of two CTAs; otherwise 128 x 128 by one.
-cudaError_t muon_launch_product(int phase, bool pair, int parity, const MuonArgs &a, const MuonTile *tiles, int n_tiles, DemoLaunch &dev, cudaStream_t stream);
+// X = S u / (||u|| + eps), as hi + lo; clears the counters of the matrices [first_mat, first_mat + n_mats) and the next task.
+cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, DemoLaunch &dev, cudaStream_t stream);
+// All products.  pair: tiles of 256 x 256 by clusters of two CTAs; otherwise 128 x 128 by one.
+cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, DemoLaunch &dev, cudaStream_t stream);
+constexpr int MUON_EPI_WARPS = 8;  // completions of a task: one for each of them in every CTA

@@ -16,12 +16,14 @@
 
 namespace {
 
-// Matrices that go through the iterations together: one launch for each product of all of them.
+// Matrices that are in the workspace together: a launch for their norms, one to lay them out and one for all their products.
 struct Group {
     int first_mat, n_mats, n_pieces;
-    bool pair;  // tiles of 256 x 256
-    long long pack_tiles, sym_tiles, full_tiles;  // first of each list
-    int n_pack, n_sym, n_full;
+    bool pair;             // tiles of 256 x 256
+    long long pack_tiles;  // first of its list
+    int n_pack;
+    long long tasks;
+    int n_tasks;
 };
 
 // Pointer arrays of an entry point: device table and mirror, uploaded when they change.
@@ -36,7 +38,7 @@ struct Tables {
 };
 enum { FROM_ORTHOGONALIZE = 0, FROM_STEP = 1, FROM_DECODE = 2, ENTRY_POINTS = 3 };
 
-constexpr long long GROUP_ELEMENTS = 32LL << 20;  // workspace: 8 bytes for each, and A and F beside them
+constexpr long long GROUP_ELEMENTS = 256LL << 20;  // workspace: 8 bytes for each, and A and F beside them
 constexpr int PRECISE_SIDE = 256;                 // up to here the products take the lo parts, too (kernels_muon.cu)
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -53,6 +55,10 @@ struct demo_muon_ctx {
     size_t bytes = 0;
     MuonMat *d_mats = nullptr;
     MuonTile *d_tiles = nullptr;
+    MuonProduct *d_products = nullptr;
+    MuonTask *d_tasks = nullptr;
+    unsigned *d_done = nullptr;  // [n_tensors] completions, the next task behind them; [n_tensors] pieces ready
+    float2 *d_scales = nullptr;
     char *d_maps = nullptr;
     char *d_work = nullptr;
     double *d_partials = nullptr;
@@ -70,6 +76,10 @@ void release(demo_muon_ctx *c)
     if (!c) return;
     cudaFree(c->d_mats);
     cudaFree(c->d_tiles);
+    cudaFree(c->d_products);
+    cudaFree(c->d_tasks);
+    cudaFree(c->d_done);
+    cudaFree(c->d_scales);
     cudaFree(c->d_maps);
     cudaFree(c->d_work);
     cudaFree(c->d_partials);
@@ -86,6 +96,8 @@ void release(demo_muon_ctx *c)
 struct Plan {
     std::vector<MuonMat> mats;
     std::vector<MuonTile> tiles;
+    std::vector<MuonProduct> products;
+    std::vector<MuonTask> tasks;
     size_t work = 0;
     int pieces = 0;
 };
@@ -98,14 +110,19 @@ size_t place(MuonMat &m, size_t at)
         at += (size_t)round_up((long long)bytes, 256);
         return reinterpret_cast<uint16_t *>(here);
     };
-    const size_t x = (size_t)m.m * (size_t)m.ldx * 2, e = (size_t)m.m * (size_t)m.lde * 2;
-    for (int p = 0; p < 2; ++p) m.xhi[p] = take(x), m.xlo[p] = take(x);
+    const size_t x = (size_t)m.m * (size_t)m.ldx * 2, e = (size_t)m.m * (size_t)m.lde * 2, rows = (size_t)round_up(m.m, 32);
+    for (int p = 0; p < 2; ++p) {
+        m.xhi[p] = take(x);
+        m.xlo[p] = m.precise ? take(x) : m.xhi[p];
+    }
     m.ehi = take(e);
     m.fhi = take(e);
     m.elo = m.precise ? take(e) : m.ehi;
     m.flo = m.precise ? take(e) : m.fhi;
-    m.d = reinterpret_cast<float *>(take((size_t)m.m * 4));
-    m.beta = reinterpret_cast<float *>(take((size_t)m.m * 4));
+    m.x32 = reinterpret_cast<float *>(take(rows * (size_t)m.ldx * 4));
+    m.e32 = reinterpret_cast<float *>(take(rows * (size_t)m.lde * 4));
+    m.d = reinterpret_cast<float *>(take((size_t)m.lde * 4));
+    m.beta = reinterpret_cast<float *>(take((size_t)m.lde * 4));
     return at;
 }
 void rebase(MuonMat &m, char *base)
@@ -119,11 +136,79 @@ void rebase(MuonMat &m, char *base)
     move(m.elo);
     move(m.fhi);
     move(m.flo);
+    move(m.x32);
+    move(m.e32);
     move(m.d);
     move(m.beta);
 }
 
 bool uses_pairs(const MuonMat &m) { return m.m > PRECISE_SIDE; }
+
+int ceil_div(int v, int by) { return (v + by - 1) / by; }
+
+// Tiles (i, j) of a grid in bands of eight rows, so that those in work together share rows and columns.
+template <class Use>
+void each_tile(int rows, int cols, bool upper, Use use)
+{
+    for (int band = 0; band < rows; band += 8)
+        for (int j = upper ? band : 0; j < cols; ++j)
+            for (int i = band; i < std::min(rows, band + 8); ++i)
+                if (!upper || i <= j) use(i, j);
+}
+
+// The products of the matrices mats[0 .. n), `first` the index of the first.  Matrices go through the iterations in cohorts, product by product,
+// every product matrix by matrix: with two rounds of the workers' tasks in a cohort's symmetric products, a matrix's next product starts when its last
+// is done, and the X of a cohort of small matrices stays in L2.
+void add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bool pair, Plan *plan)
+{
+    const int side = pair ? 256 : 128, ctas = pair ? 2 : 1, workers = std::max(1, c->launch.sm_count / ctas);
+    auto symmetric = [&](const MuonMat &m) { const long long k = ceil_div(m.m, side); return k * (k + 1) / 2; };
+    long long total = 0;
+    for (int e = 0; e < n; ++e) total += symmetric(mats[e]);
+    const long long cohorts = std::max(1LL, total / (2LL * workers));
+    long long before = 0;
+    for (int lo = 0, hi = 0; lo < n; lo = hi) {
+        const long long which = before * cohorts / total;
+        for (; hi < n && (hi == lo || before * cohorts / total == which); ++hi) before += symmetric(mats[hi]);
+        std::vector<unsigned> completed((size_t)(hi - lo), 0u);
+        for (int k = 0; k < c->cfg.steps; ++k)
+            for (int phase = MUON_GRAM; phase <= MUON_UPDATE; ++phase)
+                for (int e = lo; e < hi; ++e) {
+                    const MuonMat &m = mats[e];
+                    const int now = k & 1, x = m.maps + MUON_MAP_X0 + now, xlo = m.maps + MUON_MAP_XLO0 + now;
+                    MuonProduct t;
+                    std::memset(&t, 0, sizeof(t));
+                    t.phase = phase == MUON_UPDATE && k + 1 == c->cfg.steps ? MUON_FINAL : phase;
+                    t.mat = first + e;
+                    t.need = completed[(size_t)(e - lo)];
+                    t.steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
+                    t.parts = m.precise ? 3 : 1;
+                    t.left = phase == MUON_GRAM ? x : m.maps + (phase == MUON_POLY ? MUON_MAP_E : MUON_MAP_F);
+                    t.left_lo = phase == MUON_GRAM ? xlo : t.left + 1;
+                    t.right = phase == MUON_POLY ? t.left : x;
+                    t.right_lo = phase == MUON_POLY ? t.left_lo : xlo;
+                    t.out = m.maps + MUON_MAP_OUT + (phase == MUON_GRAM ? MUON_MAP_E : phase == MUON_POLY ? MUON_MAP_F : MUON_MAP_X0 + (now ^ 1));
+                    t.out_lo = m.maps + MUON_MAP_OUT + (phase == MUON_GRAM ? MUON_MAP_ELO : phase == MUON_POLY ? MUON_MAP_FLO : MUON_MAP_XLO0 + (now ^ 1));
+                    t.m = m.m;
+                    t.width = phase == MUON_UPDATE ? m.n : m.m;
+                    t.blocks = (phase == MUON_UPDATE ? m.ldx : m.lde) / 32;
+                    t.tensor = m.tensor;
+                    t.transposed = m.transposed;
+                    t.master = phase == MUON_UPDATE ? m.x32 : m.e32;
+                    t.vec = phase == MUON_UPDATE ? m.beta : m.d;
+                    t.beta = m.beta;
+                    t.scale = phase == MUON_GRAM ? m.inv_S * m.inv_S * MUON_EF_SCALE : m.inv_S;
+                    t.step_scale = m.step_scale * m.inv_S;
+                    const MuonTask task{(int)plan->products.size(), 0, 0};
+                    plan->products.push_back(t);
+                    const size_t begin = plan->tasks.size();
+                    each_tile(ceil_div(m.m, side), ceil_div(t.width, side), phase != MUON_UPDATE, [&](int i, int j) {
+                        plan->tasks.push_back(MuonTask{task.product, (short)i, (short)j});
+                    });
+                    completed[(size_t)(e - lo)] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(ctas * MUON_EPI_WARPS);
+                }
+    }
+}
 
 demo_status make_plan(demo_muon_ctx *c, Plan *plan)
 {
@@ -171,21 +256,12 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
         g.n_pieces = (int)pieces;
         plan->work = std::max(plan->work, work);
         plan->pieces = std::max(plan->pieces, g.n_pieces);
-        const int side = g.pair ? 256 : 128;
-        auto grid = [&](int tile_m, int tile_n, bool upper, bool square, long long *first, int *count) {
-            *first = (long long)plan->tiles.size();
-            for (size_t e = at; e < end; ++e) {
-                const MuonMat &m = all[e];
-                const int ni = (m.m + tile_m - 1) / tile_m, nj = ((square ? m.m : m.n) + tile_n - 1) / tile_n;
-                for (int i = 0; i < ni; ++i)
-                    for (int j = upper ? i : 0; j < nj; ++j) plan->tiles.push_back(MuonTile{(int)e, (short)i, (short)j});
-            }
-            *count = (int)((long long)plan->tiles.size() - *first);
-        };
-        grid(MUON_PACK_TILE, MUON_PACK_TILE, false, false, &g.pack_tiles, &g.n_pack);
-        grid(side, side, true, true, &g.sym_tiles, &g.n_sym);
-        grid(side, side, false, false, &g.full_tiles, &g.n_full);
-        if (plan->tiles.size() > (size_t)(1LL << 31) - 1) return DEMO_ERR_UNSUPPORTED;
+        g.pack_tiles = (long long)plan->tiles.size();
+        for (size_t e = at; e < end; ++e)
+            for (int i = 0; i < ceil_div(all[e].m, MUON_PACK_TILE); ++i)
+                for (int j = 0; j < ceil_div(all[e].n, MUON_PACK_TILE); ++j) plan->tiles.push_back(MuonTile{(int)e, (short)i, (short)j});
+        g.n_pack = (int)((long long)plan->tiles.size() - g.pack_tiles);
+        if (plan->tiles.size() > (size_t)(1LL << 30)) return DEMO_ERR_UNSUPPORTED;
         c->groups.push_back(g);
         at = end;
     }
@@ -193,13 +269,32 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
     return DEMO_OK;
 }
 
-bool encode_map(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, void *base, long long cols, long long rows, long long ld)
+demo_status make_tasks(demo_muon_ctx *c, Plan *plan)
 {
-    const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t gstride[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t box[2] = {64, 64}, estr[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    for (Group &g : c->groups) {
+        g.tasks = (long long)plan->tasks.size();
+        add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.pair, plan);
+        g.n_tasks = (int)((long long)plan->tasks.size() - g.tasks);
+        if (plan->tasks.size() > (size_t)(1LL << 30)) return DEMO_ERR_UNSUPPORTED;
+    }
+    return DEMO_OK;
+}
+
+// The three maps of a matrix of fp16 elements: see MUON_MAPS.
+bool encode_maps(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, void *base, long long cols, long long rows, long long ld)
+{
+    auto make = [&](CUtensorMap *to, int dims, const cuuint64_t *extent, const cuuint64_t *stride, const cuuint32_t *box, CUtensorMapSwizzle swizzle) {
+        const cuuint32_t ones[3] = {1, 1, 1};
+        return encode(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)dims, base, extent, stride, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    const cuuint64_t flat[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, row[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t panel[2] = {64, 128}, block[2] = {32, 32};
+    // blocks of 64 columns as the last axis (pad columns are read: they only reach results outside the matrix)
+    const cuuint64_t cut[3] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64)}, cut_stride[2] = {(cuuint64_t)ld * 2, 128};
+    const cuuint32_t two[3] = {64, 64, 2};
+    return make(map, 2, flat, row, panel, CU_TENSOR_MAP_SWIZZLE_128B) && make(map + MUON_MAP_MN, 3, cut, cut_stride, two, CU_TENSOR_MAP_SWIZZLE_128B) &&
+           make(map + MUON_MAP_OUT, 2, flat, row, block, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 template <typename T>
@@ -225,6 +320,8 @@ demo_status build(demo_muon_ctx *c)
     }
     const size_t T = (size_t)c->n_tensors;
     bool ok = alloc(c, &c->d_mats, T * sizeof(MuonMat)) && alloc(c, &c->d_tiles, plan.tiles.size() * sizeof(MuonTile)) &&
+              alloc(c, &c->d_done, (2 * T + 1) * sizeof(unsigned)) &&
+              alloc(c, &c->d_scales, T * sizeof(float2)) &&
               alloc(c, &c->d_maps, T * MUON_MAPS * MUON_MAP_BYTES) && alloc(c, &c->d_work, plan.work) &&
               alloc(c, &c->d_partials, (size_t)plan.pieces * sizeof(double)) && alloc(c, &c->d_status, sizeof(int));
     for (Tables &t : c->tables) {
@@ -234,21 +331,26 @@ demo_status build(demo_muon_ctx *c)
         t.out.assign(T, nullptr);
     }
     if (!ok) return DEMO_ERR_ALLOC;
+    for (MuonMat &m : plan.mats) rebase(m, c->d_work);
+    st = make_tasks(c, &plan);
+    if (st != DEMO_OK) return st;
+    if (!alloc(c, &c->d_products, plan.products.size() * sizeof(MuonProduct)) || !alloc(c, &c->d_tasks, plan.tasks.size() * sizeof(MuonTask))) return DEMO_ERR_ALLOC;
     std::vector<CUtensorMap> maps(T * MUON_MAPS);
     std::memset(maps.data(), 0, maps.size() * sizeof(CUtensorMap));
     for (MuonMat &m : plan.mats) {
-        rebase(m, c->d_work);
         CUtensorMap *p = &maps[(size_t)m.maps];
-        ok = ok && encode_map(encode, p + MUON_MAP_X0, m.xhi[0], m.n, m.m, m.ldx) && encode_map(encode, p + MUON_MAP_X1, m.xhi[1], m.n, m.m, m.ldx) &&
-             encode_map(encode, p + MUON_MAP_XLO0, m.xlo[0], m.n, m.m, m.ldx) && encode_map(encode, p + MUON_MAP_XLO1, m.xlo[1], m.n, m.m, m.ldx) &&
-             encode_map(encode, p + MUON_MAP_E, m.ehi, m.m, m.m, m.lde) && encode_map(encode, p + MUON_MAP_ELO, m.elo, m.m, m.m, m.lde) &&
-             encode_map(encode, p + MUON_MAP_F, m.fhi, m.m, m.m, m.lde) && encode_map(encode, p + MUON_MAP_FLO, m.flo, m.m, m.m, m.lde);
+        for (int x = 0; x < 2; ++x)
+            ok = ok && encode_maps(encode, p + MUON_MAP_X0 + x, m.xhi[x], m.n, m.m, m.ldx) && encode_maps(encode, p + MUON_MAP_XLO0 + x, m.xlo[x], m.n, m.m, m.ldx);
+        ok = ok && encode_maps(encode, p + MUON_MAP_E, m.ehi, m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_ELO, m.elo, m.m, m.m, m.lde) &&
+             encode_maps(encode, p + MUON_MAP_F, m.fhi, m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_FLO, m.flo, m.m, m.m, m.lde);
     }
     if (!ok) return DEMO_ERR_CUDA;
     ok = cudaMemcpy(c->d_mats, plan.mats.data(), T * sizeof(MuonMat), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_tiles, plan.tiles.data(), plan.tiles.size() * sizeof(MuonTile), cudaMemcpyHostToDevice) == cudaSuccess &&
+         cudaMemcpy(c->d_products, plan.products.data(), plan.products.size() * sizeof(MuonProduct), cudaMemcpyHostToDevice) == cudaSuccess &&
+         cudaMemcpy(c->d_tasks, plan.tasks.data(), plan.tasks.size() * sizeof(MuonTask), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice) == cudaSuccess &&
-         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess;
+         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess && cudaMemset(c->d_done, 0, (2 * T + 1) * sizeof(unsigned)) == cudaSuccess;
     return ok ? DEMO_OK : DEMO_ERR_CUDA;
 }
 
@@ -285,6 +387,10 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     a.mom = t.d_mom;
     a.out = t.d_out;
     a.partials = c->d_partials;
+    a.done = c->d_done;
+    a.next_task = c->d_done + c->n_tensors;
+    a.ready = a.next_task + 1;
+    a.scales = c->d_scales;
     a.nesterov = g.nesterov;
     a.mu = g.momentum;
     a.eps = g.eps;
@@ -296,15 +402,10 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     a.status = c->d_status;
     cudaError_t err = cudaSuccess;
     for (const Group &grp : c->groups) {
-        const MuonTile *pack = c->d_tiles + grp.pack_tiles, *sym = c->d_tiles + grp.sym_tiles, *full = c->d_tiles + grp.full_tiles;
         if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, stream);
-        if (err == cudaSuccess) err = muon_launch_pack(a, pack, grp.n_pack, c->launch, stream);
-        for (int k = 0; k < g.steps; ++k) {
-            if (err == cudaSuccess) err = muon_launch_product(MUON_GRAM, grp.pair, k & 1, a, sym, grp.n_sym, c->launch, stream);
-            if (err == cudaSuccess) err = muon_launch_product(MUON_POLY, grp.pair, k & 1, a, sym, grp.n_sym, c->launch, stream);
-            if (err == cudaSuccess) err = muon_launch_product(k + 1 < g.steps ? MUON_UPDATE : MUON_FINAL, grp.pair, k & 1, a, full, grp.n_full, c->launch, stream);
-        }
-        c->launches += 2 + 3 * g.steps;
+        if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, c->launch, stream);
+        if (err == cudaSuccess) err = muon_launch_products(grp.pair, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, c->launch, stream);
+        c->launches += 3;
     }
     if (err != cudaSuccess) {
         cudaGetLastError();
