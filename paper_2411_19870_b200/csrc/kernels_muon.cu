@@ -244,7 +244,8 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
 // ---- products -----------------------------------------------------------------------------------------------------------------
 
 constexpr int EPI_WARPS = MUON_EPI_WARPS;
-constexpr int THREADS = 64 + 32 * EPI_WARPS;  // producer warp, MMA warp, epilogue
+constexpr int SCHEDULER = EPI_WARPS + 2;       // its warp
+constexpr int THREADS = 96 + 32 * EPI_WARPS;  // loading warp, MMA warp, epilogue, scheduler
 constexpr int OPERAND = 16384;                // 128 rows (K-major) or 64 x 128 (MN-major) fp16 elements of one step of K = 64
 constexpr int STAGE = 2 * OPERAND;
 constexpr int STAGES = 6;
@@ -370,22 +371,21 @@ __device__ __forceinline__ void read_column(const float *st, int col, int q, flo
     for (int k = 0; k < 8; ++k) v[k] = st[quad_at(8 * q + k, col >> 2) + (col & 3)];
 }
 
-// Eight neighbouring results (of a tensor row, from column c on) to the caller's tensor.
-__device__ __forceinline__ void deliver(const MuonArgs &a, void *out, size_t at, int c, int cols, const float (&o)[8], float keep)
+// Eight neighbouring results (of a tensor row, from column c on) to the caller's tensor.  x: the parameters there, loaded beforehand where
+// `whole` says that they can be in 16-byte pieces.
+__device__ __forceinline__ bool whole_piece(const MuonArgs &a, int c, int cols)
 {
-    const int left = cols - c;
+    return cols - c >= 8 && (a.to == MUON_TO_OUTPUT && a.out_bf16 ? (cols & 7) == 0 : (cols & 3) == 0);
+}
+__device__ __forceinline__ void deliver(const MuonArgs &a, void *out, size_t at, int left, bool whole, const float (&o)[8], float keep, const float4 (&old)[2])
+{
     if (a.to == MUON_TO_PARAMS) {  // o = -lr s O
         float *x = static_cast<float *>(out) + at;
-        if ((cols & 3) == 0 && left >= 8) {
+        if (whole) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                float4 w = reinterpret_cast<float4 *>(x)[q];
-                w.x = fmaf(w.x, keep, o[4 * q]);
-                w.y = fmaf(w.y, keep, o[4 * q + 1]);
-                w.z = fmaf(w.z, keep, o[4 * q + 2]);
-                w.w = fmaf(w.w, keep, o[4 * q + 3]);
-                reinterpret_cast<float4 *>(x)[q] = w;
-            }
+            for (int q = 0; q < 2; ++q)
+                reinterpret_cast<float4 *>(x)[q] = make_float4(fmaf(old[q].x, keep, o[4 * q]), fmaf(old[q].y, keep, o[4 * q + 1]), fmaf(old[q].z, keep, o[4 * q + 2]),
+                                                               fmaf(old[q].w, keep, o[4 * q + 3]));
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -393,7 +393,7 @@ __device__ __forceinline__ void deliver(const MuonArgs &a, void *out, size_t at,
         }
     } else if (a.out_bf16) {
         __nv_bfloat16 *p = static_cast<__nv_bfloat16 *>(out) + at;
-        if ((cols & 7) == 0) {
+        if (whole) {
             uint32_t w[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -408,7 +408,7 @@ __device__ __forceinline__ void deliver(const MuonArgs &a, void *out, size_t at,
         }
     } else {
         float *p = static_cast<float *>(out) + at;
-        if ((cols & 3) == 0 && left >= 8) {
+        if (whole) {
             reinterpret_cast<float4 *>(p)[0] = make_float4(o[0], o[1], o[2], o[3]);
             reinterpret_cast<float4 *>(p)[1] = make_float4(o[4], o[5], o[6], o[7]);
         } else {
@@ -549,6 +549,10 @@ __device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct
     const bool params = a.to == MUON_TO_PARAMS;
     const float scale = params ? -a.lr * t.step_scale : t.scale, keep = 1.f - a.lr * a.wd;
     void *out = a.out[t.tensor];
+    // the lane's four pieces of the tensor: rows 8 i + lane / 4, eight columns; of X, where it is the transpose, the other way round
+    const int r0 = t.transposed ? b.j0 : b.r0, c = (t.transposed ? b.r0 : b.j0) + 8 * (b.lane & 3);
+    const int rows = t.transposed ? t.width : t.m, cols = t.transposed ? t.m : t.width;
+    const bool whole = whole_piece(a, c, cols);
     {
         float v[32];
         tmem_ld32(b.tmem, v);
@@ -556,20 +560,28 @@ __device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct
         for (int k = 0; k < 32; ++k) v[k] = fmaf(lin, part(x, k), v[k] * MUON_EF_INV) * scale;
         stage_rows(b.st, v, b.lane);
     }
-    __syncwarp();
-    const int sub = b.lane >> 2, q = b.lane & 3;
-#pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
-        float v[8];
-        if (t.transposed) {  // row j of the tensor is column j of X
-            const int r = b.j0 + 8 * i + sub, c = b.r0 + 8 * q;
-            read_column(b.st, 8 * i + sub, q, v);
-            if (r < t.width && c < t.m) deliver(a, out, (size_t)r * t.m + c, c, t.m, v, keep);
-        } else {
-            const int r = b.r0 + 8 * i + sub, c = b.j0 + 8 * q;
-            read_piece(b.st, 8 * i + sub, q, v);
-            if (r < t.m && c < t.width) deliver(a, out, (size_t)r * t.width + c, c, t.width, v, keep);
+    float4 old[4][2];
+    if (params && whole) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 8 * i + (b.lane >> 2);
+            if (r < rows) {
+                const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(out) + (size_t)r * cols + c);
+                old[i][0] = from[0];
+                old[i][1] = from[1];
+            }
         }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = r0 + 8 * i + (b.lane >> 2);
+        float v[8];
+        if (t.transposed)
+            read_column(b.st, 8 * i + (b.lane >> 2), b.lane & 3, v);
+        else
+            read_piece(b.st, 8 * i + (b.lane >> 2), b.lane & 3, v);
+        if (r < rows && c < cols) deliver(a, out, (size_t)r * cols + c, cols - c, whole, v, keep, old[i]);
     }
     __syncwarp();
 }
@@ -601,17 +613,18 @@ struct alignas(16) RingEntry {
 // All products of all iterations, by persistent workers (CTAs; CG = 2: pairs).  Tasks are drawn in the list's order from one counter, so
 // whatever a task waits for is done already or in the hands of a worker that runs: no worker has to be resident for another to go on.
 // One warp loads, one issues the MMAs, eight read accumulators back: two of them, so that the products of a task run beside the epilogue
-// of the one before.  The loading lane of a worker's first CTA draws the tasks and waits until they may start; those of both CTAs put
-// what the other warps need to know of one into a ring.
+// of the one before.  A fourth kind of warp schedules: that of a worker's first CTA draws the tasks and waits until they may start, and in
+// both CTAs it puts what the others need to know of one into a ring, up to four ahead (by the loading warp itself: its look-ups and waits,
+// 3500 cycles a task, leave the tensor core without data).
 // E and F are symmetric and exist above the diagonal only: left of it a panel's operand is loaded from the rows above, as its transpose.
 template <int CG>
 __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
 {
     const StreamOrder order(1);
     constexpr int TILE = 128 * CG;  // of both sides
-    constexpr int RING = 4;
+    constexpr int RING = 4, NEAR_STEPS = 8;
     extern __shared__ unsigned char raw[];
-    __shared__ unsigned long long bars[2 * STAGES + 4 + 4 * RING + 1];
+    __shared__ unsigned long long bars[2 * STAGES + 4 + 4 * RING + 2];
     __shared__ RingEntry ring[RING];
     __shared__ int drawn_ring[RING];
     __shared__ uint32_t tmem_slot;
@@ -619,7 +632,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, t_full = empty + 8 * STAGES, t_empty = t_full + 16, r_full = t_empty + 16,
-                   r_empty = r_full + 8 * RING, q_full = r_empty + 8 * RING, q_empty = q_full + 8 * RING, drained = q_empty + 8 * RING;
+                   r_empty = r_full + 8 * RING, q_full = r_empty + 8 * RING, q_empty = q_full + 8 * RING, near_end = q_empty + 8 * RING, drained = near_end + 8;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -631,10 +644,11 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
         }
         for (int s = 0; s < RING; ++s) {
             mbar_init(r_full + 8 * s, 1);
-            mbar_init(r_empty + 8 * s, EPI_WARPS + (rank == 0 ? 1 : 0));  // the epilogues and the MMA warp
+            mbar_init(r_empty + 8 * s, EPI_WARPS + (rank == 0 ? 2 : 1));  // the epilogues, the loading warp and the first CTA's MMA warp
             mbar_init(q_full + 8 * s, 1);
             mbar_init(q_empty + 8 * s, 1);
         }
+        mbar_init(near_end, 1);
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async();
@@ -661,17 +675,15 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
         if (++slot == RING) slot = 0, turn ^= 1;
     };
 
-    if (warp == 0) {
+    if (warp == SCHEDULER) {
         if (lane == 0) {
-            const uint32_t full0 = CG == 2 ? map_to_rank(full, 0) : full;
-            int stage = 0, last_product = -1;
-            unsigned phase = 0, used = 0;
+            int last_product = -1;
+            unsigned near_turn = 0;
             unsigned drawn = rank == 0 ? atomicAdd(a.next_task, 1u) : 0u;
             for (;;) {
                 int t;
                 if (rank == 0) {
                     t = drawn < (unsigned)n_tasks ? (int)drawn : -1;
-                    if (t >= 0) drawn = atomicAdd(a.next_task, 1u);  // (needed when this task's loads are under way)
                 } else {
                     ok = wait_cluster(q_full + 8 * slot, turn);
                     if (!ok) break;
@@ -687,12 +699,10 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                     for (int k = 0; k < 6; ++k) words[k] = __ldg(from + k);
                 }
                 const MuonProduct &p = *reinterpret_cast<const MuonProduct *>(words);
-                const char *left = a.maps + (size_t)p.left * MUON_MAP_BYTES, *right = a.maps + (size_t)p.right * MUON_MAP_BYTES;
-                const char *left_lo = a.maps + (size_t)p.left_lo * MUON_MAP_BYTES, *right_lo = a.maps + (size_t)p.right_lo * MUON_MAP_BYTES;
                 if (t >= 0 && tk.product != last_product) {
                     last_product = tk.product;
                     for (int lo = 0; lo < (p.parts > 1 ? 2 : 1); ++lo) {
-                        const char *l = lo ? left_lo : left, *r = lo ? right_lo : right;
+                        const char *l = a.maps + (size_t)(lo ? p.left_lo : p.left) * MUON_MAP_BYTES, *r = a.maps + (size_t)(lo ? p.right_lo : p.right) * MUON_MAP_BYTES;
                         tmap_acquire(l);
                         tmap_acquire(r);
                         if (p.phase != MUON_GRAM) {
@@ -723,11 +733,8 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 arrive(r_full + 8 * slot);
                 next_slot();
                 if (t < 0) break;
-                fence_proxy_async_all();
-                const int row = tk.i * TILE + (int)rank * 128, col = tk.j * TILE + (int)rank * 128;
-                const int left_rows = p.phase == MUON_GRAM ? 0 : tk.i * TILE;  // from here on K's elements lie in the panel's rows
-                const int right_rows = p.phase == MUON_GRAM ? 0 : p.phase == MUON_POLY ? tk.j * TILE : 1 << 30;
-                if (p.phase >= MUON_POLY) {  // the epilogue reads the tile of x32 or e32
+                const int row = tk.i * TILE + (int)rank * 128;
+                if (p.phase >= MUON_POLY) {  // the epilogue will read the tile of x32 or e32
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int b = p.blocks - tk.j * (TILE / 32);
@@ -736,9 +743,39 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                         if (row + 32 * k < p.m) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
                     }
                 }
-                for (int part = 0; ok && part < p.parts; ++part) {  // hi hi, hi lo, lo hi
+                // The next task is drawn when this one's loads are nearly through: earlier, it would only be kept from other workers.
+                if (rank == 0) {
+                    ok = wait_local(near_end, near_turn);
+                    if (!ok) break;
+                    near_turn ^= 1;
+                    drawn = atomicAdd(a.next_task, 1u);
+                }
+            }
+        }
+    } else if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t full0 = CG == 2 ? map_to_rank(full, 0) : full;
+            int stage = 0;
+            unsigned phase = 0, used = 0;
+            for (;;) {
+                ok = wait_local(r_full + 8 * slot, turn);
+                if (!ok) break;
+                const RingEntry &e = ring[slot];
+                const int end = e.end, kind = e.p.phase, steps = e.p.steps, parts = e.p.parts;
+                const char *left = a.maps + (size_t)e.p.left * MUON_MAP_BYTES, *right = a.maps + (size_t)e.p.right * MUON_MAP_BYTES;
+                const char *left_lo = a.maps + (size_t)e.p.left_lo * MUON_MAP_BYTES, *right_lo = a.maps + (size_t)e.p.right_lo * MUON_MAP_BYTES;
+                const int row = e.i * TILE + (int)rank * 128, col = e.j * TILE + (int)rank * 128;
+                const int left_rows = kind == MUON_GRAM ? 0 : e.i * TILE;  // from here on K's elements lie in the panel's rows
+                const int right_rows = kind == MUON_GRAM ? 0 : kind == MUON_POLY ? e.j * TILE : 1 << 30;
+                arrive(r_empty + 8 * slot);
+                next_slot();
+                if (end) break;
+                fence_proxy_async_all();
+                int left_steps = steps * parts;
+                for (int part = 0; ok && part < parts; ++part) {  // hi hi, hi lo, lo hi
                     const char *ml = part == 2 ? left_lo : left, *mr = part == 1 ? right_lo : right;
-                    for (int k = 0; k < p.steps; ++k) {
+                    for (int k = 0; k < steps; ++k) {
+                        if (left_steps-- == min(steps * parts, NEAR_STEPS)) arrive(near_end);
                         ok = wait_local(empty + 8 * stage, phase ^ 1);
                         if (!ok) break;
                         const uint32_t bar = full0 + 8 * stage, A = base + stage * STAGE, B = A + OPERAND;
@@ -822,16 +859,28 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
         const uint32_t t_empty0 = CG == 2 ? map_to_rank(t_empty, 0) : t_empty;
         float *st = reinterpret_cast<float *>(raw + (base - raw_s) + STAGES * STAGE) + (warp - 2) * 1024;
         int out_turn = 0;
+        unsigned *told = nullptr;  // the counter that is still to be told of this warp's last task
+        // The copies are written; with them and this warp's other stores the completion is told.  It waits for memory, so that it comes when
+        // the next task's first loads are under way, unless there is no next task yet.
+        auto tell = [&] {
+            if (lane == 0 && told) {
+                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                fence_proxy_async_all();
+                asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(told), "r"(1u) : "memory");
+            }
+            told = nullptr;
+            __syncwarp();
+        };
         for (int n_done = 0;; ++n_done) {
+            if (!__all_sync(0xffffffffu, mbar_try_wait(r_full + 8 * slot, turn))) tell();
             ok = wait_local(r_full + 8 * slot, turn);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            const MuonProduct t = ring[slot].p;
-            const int ti = ring[slot].i, tj = ring[slot].j, end = ring[slot].end;
-            __syncwarp();
-            if (lane == 0) arrive(r_empty + 8 * slot);
+            const MuonProduct &t = ring[slot].p;  // (the slot is free again when the task is done)
+            const uint32_t slot_empty = r_empty + 8 * slot;
+            const int ti = ring[slot].i, tj = ring[slot].j;
+            if (ring[slot].end) break;
             next_slot();
-            if (end) break;
             const int r0 = ti * TILE + (int)rank * 128 + q * 32, first = tj * TILE + half * (TILE / 2);
             const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 31) / 32, TILE / 64) : 0;
             const int acc = n_done & 1;
@@ -841,8 +890,15 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             if (blocks > 0 && t.phase != MUON_GRAM) {
                 load_block(master, next);
                 row = __ldcg(t.vec + r0 + lane);
-                if (t.phase != MUON_POLY) row += a.a;
             }
+            if (t.phase == MUON_FINAL && a.to == MUON_TO_PARAMS) {  // the parameters' rows on their way to L2
+                const int rows = t.transposed ? t.width : t.m, cols = t.transposed ? t.m : t.width;
+                for (int b = 0; b < blocks; ++b) {
+                    const int r = (t.transposed ? first + 32 * b : r0) + lane, c = t.transposed ? r0 : first + 32 * b;
+                    if (r < rows) prefetch_l2(static_cast<const float *>(a.out[t.tensor]) + (size_t)r * cols + c);
+                }
+            }
+            tell();
             ok = wait_local(t_full + 8 * acc, (n_done >> 1) & 1);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -861,9 +917,9 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             else if (t.phase == MUON_POLY)
                 each_block([&](const BlockAt &b) { block_poly(a, t, b, out_turn, x, row); });
             else if (t.phase == MUON_UPDATE)
-                each_block([&](const BlockAt &b) { block_update(a, t, b, out_turn, x, row); });
+                each_block([&](const BlockAt &b) { block_update(a, t, b, out_turn, x, a.a + row); });
             else
-                each_block([&](const BlockAt &b) { block_final(a, t, b, x, row); });
+                each_block([&](const BlockAt &b) { block_final(a, t, b, x, a.a + row); });
             tc_before();
             __syncwarp();
             if (lane == 0) {
@@ -871,15 +927,12 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                     arrive_cluster(t_empty0 + 8 * acc);
                 else
                     arrive(t_empty0 + 8 * acc);
-                if (t.phase != MUON_FINAL) {
-                    // the copies are written; with them and this warp's other stores the completion is told
-                    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-                    fence_proxy_async_all();
-                    asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a.done + t.mat), "r"(1u) : "memory");
-                }
             }
+            if (t.phase != MUON_FINAL) told = a.done + t.mat;
             __syncwarp();
+            if (lane == 0) arrive(slot_empty);
         }
+        tell();
     }
     if (!ok) atomicExch(a.status, DEMO_DEV_TIMEOUT);
     __syncwarp();
