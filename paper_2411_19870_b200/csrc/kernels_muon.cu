@@ -3,17 +3,21 @@
 //   X_0 = u / (||u||_F + eps);  A = X X^T;  X <- a X + (b A + c A^2) X
 //
 // as three products an iteration, the tasks of one persistent kernel:
-//   GRAM    A = X X^T        symmetric: the tiles on and above the diagonal, mirrored
-//   POLY    A^2 -> F, beta   symmetric, too
-//   UPDATE  F X  -> X
+//   GRAM    A = X X^T                        symmetric: the tiles on and above the diagonal
+//   POLY    B = a + b A + c A^2, from A^2     symmetric, too
+//   UPDATE  X <- B X
+// Wide matrices do two iterations in one: the second's A is A B^2, a polynomial of the first's, and X <- (B' B) X is multiplied once,
+//   GRAM, POLY, MUL T = A B, MUL A' = T B, POLY B', MUL Q = B' B, UPDATE
+// which for n = 4 m takes 17 m^3 instead of 26 and reads and writes X once.
 // Operands are fp16 (11 bits, accumulated in fp32), and what would lose accuracy in them is kept out of them:
-//   * the linear term a X, on which small singular values live alone (they grow by a = 3.4 an iteration, rounding noise with them),
-//     is formed from X = hi + lo, 22 bits;
-//   * the diagonal of A, of order one in the last iterations, where a X and (b A + c A^2) X nearly cancel, never passes through fp16:
-//     A = D + E, A^2 = D^2 + D E + E D + E^2, so F = offdiag((b + c (d_i + d_j)) E + c E^2) and X <- (a + beta_i) X + F X with
-//     beta_i = b d_i + c (d_i^2 + (E^2)_ii) in fp32.
-// Relative error of the result against 64 bits, Gaussian 1024 x 1024: 6e-4 (plain fp16 operands 1.6e-3, bf16 1.2e-2); of rank one:
-// 5e-4 (0.15 and 1.2).  It grows as matrices shrink, so those of up to 256 rows take the lo parts of the products' operands, too.
+//   * the linear term, on which small singular values live alone (they grow by a = 3.4 an iteration, rounding noise with them), and all
+//     other sums outside the products are formed from fp32 copies;
+//   * the diagonals of symmetric matrices, of order one in the last iterations, where a X and (b A + c A^2) X nearly cancel, never pass
+//     through fp16: with P = D + E, Q = D' + E', P Q = D D' + D E' + E D' + E E', and only E E' is a product on the tensor cores.
+// Relative error of the result against 64 bits, 1024 x 4096: Gaussian 2e-4, of rank one 8e-4, of rank 32 2e-3 (plain bf16 operands, one
+// iteration after the other: 1.3e-2, 1.2 and 0.2; fp16: 1.7e-3, 0.15 and 0.03).  It grows as matrices shrink, so those of up to 256 rows take
+// the lo parts of the products' operands, too.  All five iterations in one would take 29 m^3 for n = 4 m, where two at a time take 47, but
+// noise outside a low rank then grows to 0.15: B' B of two iterations is at most a^2 = 12, of five 480, and is rounded to 11 bits.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -428,10 +432,21 @@ __device__ __forceinline__ void stage_halves(unsigned char *buf, const uint32_t 
     for (int c = 0; c < 4; ++c)
         *reinterpret_cast<uint4 *>(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
 }
+struct BlockAt {
+    const float *src2;  // the lane's place in the block of the right factor's fp32 copy
+    float *dst;         // and of the result's
+    uint32_t tmem;
+    int r0, j0, lane;
+    float *st;          // the warp's 4 KB of shared memory
+};
+
 // Writes a block as fp16 and, where the products need it, what that leaves.  The copies read the buffers after this returns; two alternate.
 // (pad columns and rows: the copy leaves out what lies outside the matrix)
-__device__ __forceinline__ void write_halves(unsigned char *bufs, int &turn, const char *map, const char *map_lo, bool precise, const float (&v)[32], int r0, int j0, int lane)
+__device__ __forceinline__ void write_halves(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float (&v)[32])
 {
+    const bool precise = t.parts > 1;
+    const int lane = b.lane;
+    unsigned char *bufs = reinterpret_cast<unsigned char *>(b.st);
     uint32_t p[16];
 #pragma unroll
     for (int k = 0; k < 16; ++k) p[k] = pack2(v[2 * k], v[2 * k + 1]);
@@ -456,8 +471,8 @@ __device__ __forceinline__ void write_halves(unsigned char *bufs, int &turn, con
     fence_proxy_async();
     __syncwarp();
     if (lane == 0) {
-        tma_store_2d(map, j0, r0, smem_u32(buf));
-        if (precise) tma_store_2d(map_lo, j0, r0, smem_u32(bufs + 2048));
+        tma_store_2d(a.maps + (size_t)t.out * MUON_MAP_BYTES, b.j0, b.r0, smem_u32(buf));
+        if (precise) tma_store_2d(a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, b.j0, b.r0, smem_u32(bufs + 2048));
         tma_store_commit();
     }
 }
@@ -468,6 +483,12 @@ __device__ __forceinline__ void load_block(const float *p, float4 (&x)[8])
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(p + k * 128));
 }
+// 32 elements of a vector, the same for all lanes
+__device__ __forceinline__ void load_vector(const float *p, float4 (&x)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(p) + k);
+}
 __device__ __forceinline__ void store_block(float *p, const float (&v)[32])
 {
 #pragma unroll
@@ -475,76 +496,75 @@ __device__ __forceinline__ void store_block(float *p, const float (&v)[32])
 }
 __device__ __forceinline__ const float &part(const float4 (&x)[8], int k) { return reinterpret_cast<const float *>(x)[k]; }
 
-struct BlockAt {
-    float *master;  // the lane's place in the block
-    uint32_t tmem;
-    int r0, j0, lane;
-    float *st;      // the warp's 4 KB of shared memory
-};
+// Is this block on the diagonal, its lane's own element is v[lane]: `own` takes it, and zero comes in its place.
+__device__ __forceinline__ float take_own(float (&v)[32], int lane)
+{
+    float own = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+        if (k == lane) {
+            own = v[k];
+            v[k] = 0.f;
+        }
+    return own;
+}
 
-// E = A off the diagonal, d on it.
 __device__ __forceinline__ void block_gram(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn)
 {
     float v[32];
     tmem_ld32(b.tmem, v);
 #pragma unroll
     for (int k = 0; k < 32; ++k) v[k] *= t.scale;
-    if (b.r0 == b.j0) {
-        float d = 0.f;
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-            if (k == b.lane) {
-                d = v[k];
-                v[k] = 0.f;
-            }
-        __stcg(t.vec + b.r0 + b.lane, d * MUON_EF_INV);
-    }
-    store_block(b.master, v);
-    write_halves(reinterpret_cast<unsigned char *>(b.st), turn, a.maps + (size_t)t.out * MUON_MAP_BYTES, a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, t.parts > 1, v, b.r0, b.j0,
-                 b.lane);
+    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, take_own(v, b.lane) * MUON_EF_INV);
+    store_block(b.dst, v);
+    write_halves(a, t, b, turn, v);
 }
 
-// F = (b + c (d_i + d_j)) E + c E^2 off the diagonal, beta = b d + c (d^2 + E^2) on it.
+// B = a + b A + c A^2
 __device__ __forceinline__ void block_poly(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&e)[8], float di)
 {
     float v[32];
     float4 dj[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) dj[k] = __ldcg(reinterpret_cast<const float4 *>(t.vec + b.j0) + k);
+    load_vector(t.vec + b.j0, dj);
     tmem_ld32(b.tmem, v);
-    if (b.r0 == b.j0) {
-        float square = 0.f;
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-            if (k == b.lane) square = v[k];
-        __stcg(t.beta + b.r0 + b.lane, fmaf(a.b, di, a.c * fmaf(di, di, square * (MUON_EF_INV * MUON_EF_INV))));
-    }
+    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, a.a + fmaf(a.b, di, a.c * fmaf(di, di, take_own(v, b.lane) * (MUON_EF_INV * MUON_EF_INV))));
     const float base = fmaf(a.c, di, a.b), scale = a.c * MUON_EF_INV;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(fmaf(a.c, part(dj, k), base), part(e, k), scale * v[k]);
-    if (b.r0 == b.j0) {
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-            if (k == b.lane) v[k] = 0.f;
-    }
-    write_halves(reinterpret_cast<unsigned char *>(b.st), turn, a.maps + (size_t)t.out * MUON_MAP_BYTES, a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, t.parts > 1, v, b.r0, b.j0,
-                 b.lane);
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(fmaf(a.c, part(dj, k), base), part(e, k), scale * v[k]);  // (E's own diagonal is zero)
+    if (t.dst) store_block(b.dst, v);
+    write_halves(a, t, b, turn, v);
 }
 
-// X <- (a + beta) X + F X
-__device__ __forceinline__ void block_update(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&x)[8], float lin)
+// P Q, of matrices that commute
+__device__ __forceinline__ void block_mul(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&e)[8], float di)
+{
+    float v[32];
+    float4 f[8];
+    load_block(b.src2, f);
+    tmem_ld32(b.tmem, v);
+    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, fmaf(di, __ldcg(t.vec2 + b.r0 + b.lane), take_own(v, b.lane) * (MUON_EF_INV * MUON_EF_INV)));
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(f, k), v[k] * MUON_EF_INV);
+    load_vector(t.vec2 + b.j0, f);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(part(e, k), part(f, k), v[k]);
+    if (t.dst) store_block(b.dst, v);
+    write_halves(a, t, b, turn, v);
+}
+
+// X <- B X
+__device__ __forceinline__ void block_update(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&x)[8], float di)
 {
     float v[32];
     tmem_ld32(b.tmem, v);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(lin, part(x, k), v[k] * MUON_EF_INV);
-    store_block(b.master, v);
-    write_halves(reinterpret_cast<unsigned char *>(b.st), turn, a.maps + (size_t)t.out * MUON_MAP_BYTES, a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, t.parts > 1, v, b.r0, b.j0,
-                 b.lane);
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV);
+    store_block(b.dst, v);
+    write_halves(a, t, b, turn, v);
 }
 
 // The same, the last time: to the caller's tensor.
-__device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, const float4 (&x)[8], float lin)
+__device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, const float4 (&x)[8], float di)
 {
     const bool params = a.to == MUON_TO_PARAMS;
     const float scale = params ? -a.lr * t.step_scale : t.scale, keep = 1.f - a.lr * a.wd;
@@ -557,7 +577,7 @@ __device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct
         float v[32];
         tmem_ld32(b.tmem, v);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = fmaf(lin, part(x, k), v[k] * MUON_EF_INV) * scale;
+        for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV) * scale;
         stage_rows(b.st, v, b.lane);
     }
     float4 old[4][2];
@@ -616,7 +636,7 @@ struct alignas(16) RingEntry {
 // of the one before.  A fourth kind of warp schedules: that of a worker's first CTA draws the tasks and waits until they may start, and in
 // both CTAs it puts what the others need to know of one into a ring, up to four ahead (by the loading warp itself: its look-ups and waits,
 // 3500 cycles a task, leave the tensor core without data).
-// E and F are symmetric and exist above the diagonal only: left of it a panel's operand is loaded from the rows above, as its transpose.
+// Symmetric matrices exist above the diagonal only: left of it a panel's operand is loaded from the rows above, as its transpose.
 template <int CG>
 __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
 {
@@ -692,11 +712,11 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 }
                 MuonTask tk{0, 0, 0};
                 if (t >= 0) tk = tasks[t];
-                uint4 words[6];
+                uint4 words[8];
                 {
                     const uint4 *from = reinterpret_cast<const uint4 *>(products + tk.product);
 #pragma unroll
-                    for (int k = 0; k < 6; ++k) words[k] = __ldg(from + k);
+                    for (int k = 0; k < 8; ++k) words[k] = __ldg(from + k);
                 }
                 const MuonProduct &p = *reinterpret_cast<const MuonProduct *>(words);
                 if (t >= 0 && tk.product != last_product) {
@@ -727,22 +747,22 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 {
                     uint4 *to = reinterpret_cast<uint4 *>(ring + slot);
 #pragma unroll
-                    for (int k = 0; k < 6; ++k) to[k] = words[k];
-                    to[6] = make_uint4((unsigned)(int)tk.i, (unsigned)(int)tk.j, t < 0 ? 1u : 0u, 0u);
+                    for (int k = 0; k < 8; ++k) to[k] = words[k];
+                    to[8] = make_uint4((unsigned)(int)tk.i, (unsigned)(int)tk.j, t < 0 ? 1u : 0u, 0u);
                 }
                 arrive(r_full + 8 * slot);
                 next_slot();
                 if (t < 0) break;
                 const int row = tk.i * TILE + (int)rank * 128;
-                if (p.phase >= MUON_POLY) {  // the epilogue will read the tile of x32 or e32
+                // the epilogue will read the tile of the fp32 copies
+                for (int f = 0; f < (p.phase == MUON_GRAM ? 0 : p.phase == MUON_MUL ? 2 : 1); ++f)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int b = p.blocks - tk.j * (TILE / 32);
                         const unsigned bytes = (unsigned)(b < TILE / 32 ? b : TILE / 32) * 4096u;
-                        const float *at = p.master + ((size_t)(row / 32 + k) * p.blocks + tk.j * (TILE / 32)) * 1024;
+                        const float *at = (f ? p.src2 : p.src) + ((size_t)(row / 32 + k) * p.blocks + tk.j * (TILE / 32)) * 1024;
                         if (row + 32 * k < p.m) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
                     }
-                }
                 // The next task is drawn when this one's loads are nearly through: earlier, it would only be kept from other workers.
                 if (rank == 0) {
                     ok = wait_local(near_end, near_turn);
@@ -766,7 +786,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 const char *left_lo = a.maps + (size_t)e.p.left_lo * MUON_MAP_BYTES, *right_lo = a.maps + (size_t)e.p.right_lo * MUON_MAP_BYTES;
                 const int row = e.i * TILE + (int)rank * 128, col = e.j * TILE + (int)rank * 128;
                 const int left_rows = kind == MUON_GRAM ? 0 : e.i * TILE;  // from here on K's elements lie in the panel's rows
-                const int right_rows = kind == MUON_GRAM ? 0 : kind == MUON_POLY ? e.j * TILE : 1 << 30;
+                const int right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? e.j * TILE : 1 << 30;
                 arrive(r_empty + 8 * slot);
                 next_slot();
                 if (end) break;
@@ -811,7 +831,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 if (!ok) break;
                 const RingEntry &e = ring[slot];
                 const int end = e.end, kind = e.p.phase, steps = e.p.steps, parts = e.p.parts;
-                const int left_rows = kind == MUON_GRAM ? 0 : e.i * TILE, right_rows = kind == MUON_GRAM ? 0 : kind == MUON_POLY ? e.j * TILE : 1 << 30;
+                const int left_rows = kind == MUON_GRAM ? 0 : e.i * TILE, right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? e.j * TILE : 1 << 30;
                 arrive(r_empty + 8 * slot);
                 next_slot();
                 if (end) break;
@@ -884,11 +904,11 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             const int r0 = ti * TILE + (int)rank * 128 + q * 32, first = tj * TILE + half * (TILE / 2);
             const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 31) / 32, TILE / 64) : 0;
             const int acc = n_done & 1;
-            float *master = t.master + ((size_t)(r0 / 32) * t.blocks + first / 32) * 1024 + lane * 4;
+            const size_t at = ((size_t)(r0 / 32) * t.blocks + first / 32) * 1024 + lane * 4;
             float4 x[8], next[8];
             float row = 0.f;
             if (blocks > 0 && t.phase != MUON_GRAM) {
-                load_block(master, next);
+                load_block(t.src + at, next);
                 row = __ldcg(t.vec + r0 + lane);
             }
             if (t.phase == MUON_FINAL && a.to == MUON_TO_PARAMS) {  // the parameters' rows on their way to L2
@@ -908,18 +928,20 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 for (int b = 0; b < blocks; ++b) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) x[k] = next[k];
-                    if (t.phase != MUON_GRAM && b + 1 < blocks) load_block(master + (b + 1) * 1024, next);
-                    use(BlockAt{master + b * 1024, tmem + acc * 256 + half * (TILE / 2) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, st});
+                    if (t.phase != MUON_GRAM && b + 1 < blocks) load_block(t.src + at + (b + 1) * 1024, next);
+                    use(BlockAt{t.src2 + at + b * 1024, t.dst + at + b * 1024, tmem + acc * 256 + half * (TILE / 2) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, st});
                 }
             };
             if (t.phase == MUON_GRAM)
                 each_block([&](const BlockAt &b) { block_gram(a, t, b, out_turn); });
             else if (t.phase == MUON_POLY)
                 each_block([&](const BlockAt &b) { block_poly(a, t, b, out_turn, x, row); });
+            else if (t.phase == MUON_MUL)
+                each_block([&](const BlockAt &b) { block_mul(a, t, b, out_turn, x, row); });
             else if (t.phase == MUON_UPDATE)
-                each_block([&](const BlockAt &b) { block_update(a, t, b, out_turn, x, a.a + row); });
+                each_block([&](const BlockAt &b) { block_update(a, t, b, out_turn, x, row); });
             else
-                each_block([&](const BlockAt &b) { block_final(a, t, b, x, a.a + row); });
+                each_block([&](const BlockAt &b) { block_final(a, t, b, x, row); });
             tc_before();
             __syncwarp();
             if (lane == 0) {

@@ -18,11 +18,11 @@ demo_status demo_decode_momentum(demo_ctx *ctx, const void *const *payloads, int
                                  size_t momentum_bytes, cudaStream_t stream);
 
 // One matrix.  The kernels work on X with `m` <= `n`: a tensor with more rows than columns is held transposed.  In the workspace, scaled by
-// the power of two `S`:
-//   X     fp16 (twice: an iteration reads one and writes the other; lo parts only for `precise` matrices), rows of `ldx` elements, and x32, fp32
-//   A     its diagonal d; the rest, E = A - D, fp16, rows of `lde` elements, and e32, fp32.  Only tiles on and above the diagonal exist.
-//   F, beta  the polynomial of A, split the same way
-// x32 and e32 lie in blocks of 32 x 32 as the epilogues' lanes hold them: eight groups of four columns, in each 32 rows of four elements.
+// the power of two `S`, X is fp16 (twice: a product reads one and writes the other; lo parts only for `precise` matrices), rows of `ldx`
+// elements, and x32, fp32.  Beside it are two or three symmetric matrices, A = X X^T and polynomials of it, each as its diagonal (fp32) and
+// the rest: fp16, rows of `lde` elements, and fp32.  Only tiles on and above the diagonal exist.
+// The fp32 copies lie in blocks of 32 x 32 as the epilogues' lanes hold them: eight groups of four columns, in each 32 rows of four elements.
+constexpr int MUON_SYMMETRIC = 3;
 struct MuonMat {
     int m, n;
     int ldx, lde;      // multiples of 64
@@ -34,18 +34,19 @@ struct MuonMat {
     int maps;          // index of its first tensor map (MUON_MAPS of them)
     float S, inv_S;
     float step_scale;  // of the update: x <- x - lr (step_scale O + wd x)
+    int symmetric;     // how many symmetric matrices
     uint16_t *xhi[2], *xlo[2];
-    uint16_t *ehi, *elo, *fhi, *flo;
-    float *x32, *e32;
-    float *d, *beta;
+    uint16_t *ehi[MUON_SYMMETRIC], *elo[MUON_SYMMETRIC];
+    float *x32, *e32[MUON_SYMMETRIC], *diag[MUON_SYMMETRIC];
 };
-// Tensor maps of a matrix, three of each of these: boxes of 128 rows x 64 columns (an operand whose rows run along K), two of 64 x 64 side
-// by side (one whose columns do), both with 128-byte swizzle, and 32 x 32 with 64-byte swizzle (what an epilogue writes).
-enum { MUON_MAP_X0 = 0, MUON_MAP_X1 = 1, MUON_MAP_XLO0 = 2, MUON_MAP_XLO1 = 3, MUON_MAP_E = 4, MUON_MAP_ELO = 5, MUON_MAP_F = 6, MUON_MAP_FLO = 7 };
-constexpr int MUON_MAP_MN = 8, MUON_MAP_OUT = 16, MUON_MAPS = 24;
+// Tensor maps of a matrix (X twice, its lo parts, the symmetric matrices, theirs), three of each: boxes of 128 rows x 64 columns (an operand
+// whose rows run along K), two of 64 x 64 side by side (one whose columns do), both with 128-byte swizzle, and 32 x 32 with 64-byte swizzle
+// (what an epilogue writes).
+enum { MUON_MAP_X = 0, MUON_MAP_XLO = 2, MUON_MAP_E = 4, MUON_MAP_ELO = 4 + MUON_SYMMETRIC, MUON_MAP_KINDS = 4 + 2 * MUON_SYMMETRIC };
+constexpr int MUON_MAP_MN = MUON_MAP_KINDS, MUON_MAP_OUT = 2 * MUON_MAP_KINDS, MUON_MAPS = 3 * MUON_MAP_KINDS;
 constexpr int MUON_MAP_BYTES = 128;
 
-// E and F lie in the workspace 256 times as large: entries of 1/m and less, and their lo parts, stay in fp16's normal range (of rank one,
+// Off the diagonal, symmetric matrices lie in the workspace 256 times as large: entries of 1/m and less, and their lo parts, stay in fp16's normal range (of rank one,
 // 96 rows: error 1.6e-4 without).  Entries of up to 255 remain possible: singular values up to about 3 within the iterations.
 constexpr float MUON_EF_SCALE = 256.f, MUON_EF_INV = 1.f / 256.f;
 
@@ -59,7 +60,7 @@ struct MuonTile {
 
 // The products of all matrices are one list of tasks, a tile each; workers draw them in order, so a task may wait for what earlier ones
 // write: `need` completions of its matrix's (each warp of an epilogue is one).
-enum { MUON_GRAM = 0, MUON_POLY = 1, MUON_UPDATE = 2, MUON_FINAL = 3 };
+enum { MUON_GRAM = 0, MUON_POLY = 1, MUON_MUL = 2, MUON_UPDATE = 3, MUON_FINAL = 4 };
 struct MuonTask {
     int product;
     short i, j;
@@ -74,12 +75,16 @@ struct alignas(16) MuonProduct {  // what the tasks of one product of one matrix
     int blocks;              // of x32 / e32 in a row of them
     int m, width;            // of the result
     int tensor, transposed;
-    float *master;           // e32 (written by GRAM, read by POLY), x32
-    float *vec;              // d (GRAM writes it, POLY reads it), beta
-    float *beta;             // POLY: written
-    float scale, step_scale; // GRAM: of E; FINAL: of O, of the update
+    const float *src;        // fp32: POLY, MUL: the left factor; UPDATE, FINAL: X
+    const float *src2;       // MUL: the right factor
+    float *dst;              // fp32 result, NULL: not needed
+    const float *vec;        // POLY, MUL: the left factor's diagonal; UPDATE, FINAL: the polynomial's
+    const float *vec2;       // MUL: the right factor's diagonal
+    float *diag;             // the result's diagonal
+    float scale, step_scale; // GRAM: of A off the diagonal; FINAL: of O, of the update
+    int pad[2];
 };
-static_assert(sizeof(MuonProduct) == 96, "read as six 16-byte pieces");
+static_assert(sizeof(MuonProduct) == 128, "read as eight 16-byte pieces");
 
 // What the update is formed from and what becomes of it.
 enum { MUON_FROM_STEP = 0, MUON_FROM_INPUT = 1 };   // u = g + mu m' (or m'), m' = mu m + g; or u = the input itself

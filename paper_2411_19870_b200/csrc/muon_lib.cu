@@ -115,14 +115,13 @@ size_t place(MuonMat &m, size_t at)
         m.xhi[p] = take(x);
         m.xlo[p] = m.precise ? take(x) : m.xhi[p];
     }
-    m.ehi = take(e);
-    m.fhi = take(e);
-    m.elo = m.precise ? take(e) : m.ehi;
-    m.flo = m.precise ? take(e) : m.fhi;
     m.x32 = reinterpret_cast<float *>(take(rows * (size_t)m.ldx * 4));
-    m.e32 = reinterpret_cast<float *>(take(rows * (size_t)m.lde * 4));
-    m.d = reinterpret_cast<float *>(take((size_t)m.lde * 4));
-    m.beta = reinterpret_cast<float *>(take((size_t)m.lde * 4));
+    for (int k = 0; k < m.symmetric; ++k) {
+        m.ehi[k] = take(e);
+        m.elo[k] = m.precise ? take(e) : m.ehi[k];
+        m.e32[k] = reinterpret_cast<float *>(take(rows * (size_t)m.lde * 4));
+        m.diag[k] = reinterpret_cast<float *>(take((size_t)m.lde * 4));
+    }
     return at;
 }
 void rebase(MuonMat &m, char *base)
@@ -132,17 +131,19 @@ void rebase(MuonMat &m, char *base)
         move(m.xhi[p]);
         move(m.xlo[p]);
     }
-    move(m.ehi);
-    move(m.elo);
-    move(m.fhi);
-    move(m.flo);
     move(m.x32);
-    move(m.e32);
-    move(m.d);
-    move(m.beta);
+    for (int k = 0; k < m.symmetric; ++k) {
+        move(m.ehi[k]);
+        move(m.elo[k]);
+        move(m.e32[k]);
+        move(m.diag[k]);
+    }
 }
 
 bool uses_pairs(const MuonMat &m) { return m.m > PRECISE_SIDE; }
+
+// Two iterations in one (kernels_muon.cu) take 3 r + 5 products of m^3 multiplications, one after the other 6 r + 2, r = n / m.
+bool in_twos(const MuonMat &m, int steps) { return !m.precise && steps >= 3 && 2LL * m.n >= 3LL * m.m; }
 
 int ceil_div(int v, int by) { return (v + by - 1) / by; }
 
@@ -154,6 +155,79 @@ void each_tile(int rows, int cols, bool upper, Use use)
         for (int j = upper ? band : 0; j < cols; ++j)
             for (int i = band; i < std::min(rows, band + 8); ++i)
                 if (!upper || i <= j) use(i, j);
+}
+
+// The products that one matrix goes through, in order.
+std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
+{
+    std::vector<MuonProduct> list;
+    int now = 0;  // the X that is read
+    auto add = [&](int phase) -> MuonProduct & {
+        MuonProduct t;
+        std::memset(&t, 0, sizeof(t));
+        const bool wide = phase >= MUON_UPDATE;
+        t.phase = phase;
+        t.steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
+        t.parts = m.precise ? 3 : 1;
+        t.m = m.m;
+        t.width = wide ? m.n : m.m;
+        t.blocks = (wide ? m.ldx : m.lde) / 32;
+        t.tensor = m.tensor;
+        t.transposed = m.transposed;
+        t.scale = phase == MUON_GRAM ? m.inv_S * m.inv_S * MUON_EF_SCALE : m.inv_S;
+        t.step_scale = m.step_scale * m.inv_S;
+        list.push_back(t);
+        return list.back();
+    };
+    auto x_maps = [&](int &hi, int &lo, int which) { hi = m.maps + MUON_MAP_X + which, lo = m.maps + MUON_MAP_XLO + which; };
+    auto e_maps = [&](int &hi, int &lo, int which) { hi = m.maps + MUON_MAP_E + which, lo = m.maps + MUON_MAP_ELO + which; };
+    auto result = [&](MuonProduct &t, int to, bool fp32) {
+        e_maps(t.out, t.out_lo, to);
+        t.dst = fp32 ? m.e32[to] : nullptr;
+        t.diag = m.diag[to];
+    };
+    auto gram = [&](int to) {
+        MuonProduct &t = add(MUON_GRAM);
+        x_maps(t.left, t.left_lo, now);
+        x_maps(t.right, t.right_lo, now);
+        result(t, to, true);
+    };
+    auto multiply = [&](int phase, int p, int q, int to, bool fp32) {
+        MuonProduct &t = add(phase);
+        e_maps(t.left, t.left_lo, p);
+        e_maps(t.right, t.right_lo, q);
+        t.src = m.e32[p];
+        t.src2 = m.e32[q];
+        t.vec = m.diag[p];
+        t.vec2 = m.diag[q];
+        result(t, to, fp32);
+    };
+    auto update = [&](int by, bool last) {
+        MuonProduct &t = add(last ? MUON_FINAL : MUON_UPDATE);
+        e_maps(t.left, t.left_lo, by);
+        x_maps(t.right, t.right_lo, now);
+        t.src = t.dst = m.x32;
+        t.vec = m.diag[by];
+        now ^= 1;
+        x_maps(t.out, t.out_lo, now);
+    };
+    for (int k = 0; k < steps;) {
+        // the first alone: [1, 2, 2] has a third of the error of [2, 2, 1] where the rank is low
+        const bool two = in_twos(m, steps) && k > 0 && k + 2 <= steps;
+        gram(0);
+        multiply(MUON_POLY, 0, 0, 1, two);
+        if (two) {
+            multiply(MUON_MUL, 0, 1, 2, true);   // T = A B
+            multiply(MUON_MUL, 2, 1, 0, true);   // A' = T B
+            multiply(MUON_POLY, 0, 0, 2, true);  // B'
+            multiply(MUON_MUL, 2, 1, 0, false);  // Q = B' B
+        }
+        k += two ? 2 : 1;
+        update(two ? 0 : 1, k == steps);
+    }
+    for (MuonProduct &t : list)
+        for (int *map : {&t.out, &t.out_lo}) *map += MUON_MAP_OUT;
+    return list;
 }
 
 // The products of the matrices mats[0 .. n), `first` the index of the first.  Matrices go through the iterations in cohorts, product by product,
@@ -170,43 +244,25 @@ void add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bo
     for (int lo = 0, hi = 0; lo < n; lo = hi) {
         const long long which = before * cohorts / total;
         for (; hi < n && (hi == lo || before * cohorts / total == which); ++hi) before += symmetric(mats[hi]);
-        std::vector<unsigned> completed((size_t)(hi - lo), 0u);
-        for (int k = 0; k < c->cfg.steps; ++k)
-            for (int phase = MUON_GRAM; phase <= MUON_UPDATE; ++phase)
-                for (int e = lo; e < hi; ++e) {
-                    const MuonMat &m = mats[e];
-                    const int now = k & 1, x = m.maps + MUON_MAP_X0 + now, xlo = m.maps + MUON_MAP_XLO0 + now;
-                    MuonProduct t;
-                    std::memset(&t, 0, sizeof(t));
-                    t.phase = phase == MUON_UPDATE && k + 1 == c->cfg.steps ? MUON_FINAL : phase;
-                    t.mat = first + e;
-                    t.need = completed[(size_t)(e - lo)];
-                    t.steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
-                    t.parts = m.precise ? 3 : 1;
-                    t.left = phase == MUON_GRAM ? x : m.maps + (phase == MUON_POLY ? MUON_MAP_E : MUON_MAP_F);
-                    t.left_lo = phase == MUON_GRAM ? xlo : t.left + 1;
-                    t.right = phase == MUON_POLY ? t.left : x;
-                    t.right_lo = phase == MUON_POLY ? t.left_lo : xlo;
-                    t.out = m.maps + MUON_MAP_OUT + (phase == MUON_GRAM ? MUON_MAP_E : phase == MUON_POLY ? MUON_MAP_F : MUON_MAP_X0 + (now ^ 1));
-                    t.out_lo = m.maps + MUON_MAP_OUT + (phase == MUON_GRAM ? MUON_MAP_ELO : phase == MUON_POLY ? MUON_MAP_FLO : MUON_MAP_XLO0 + (now ^ 1));
-                    t.m = m.m;
-                    t.width = phase == MUON_UPDATE ? m.n : m.m;
-                    t.blocks = (phase == MUON_UPDATE ? m.ldx : m.lde) / 32;
-                    t.tensor = m.tensor;
-                    t.transposed = m.transposed;
-                    t.master = phase == MUON_UPDATE ? m.x32 : m.e32;
-                    t.vec = phase == MUON_UPDATE ? m.beta : m.d;
-                    t.beta = m.beta;
-                    t.scale = phase == MUON_GRAM ? m.inv_S * m.inv_S * MUON_EF_SCALE : m.inv_S;
-                    t.step_scale = m.step_scale * m.inv_S;
-                    const MuonTask task{(int)plan->products.size(), 0, 0};
-                    plan->products.push_back(t);
-                    const size_t begin = plan->tasks.size();
-                    each_tile(ceil_div(m.m, side), ceil_div(t.width, side), phase != MUON_UPDATE, [&](int i, int j) {
-                        plan->tasks.push_back(MuonTask{task.product, (short)i, (short)j});
-                    });
-                    completed[(size_t)(e - lo)] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(ctas * MUON_EPI_WARPS);
-                }
+        std::vector<std::vector<MuonProduct>> lists;
+        for (int e = lo; e < hi; ++e) lists.push_back(products_of(mats[e], c->cfg.steps));
+        std::vector<unsigned> completed(lists.size(), 0u);
+        for (size_t k = 0, more = 1; more; ++k) {
+            more = 0;
+            for (size_t e = 0; e < lists.size(); ++e) {
+                if (k >= lists[e].size()) continue;
+                more = 1;
+                MuonProduct t = lists[e][k];
+                t.mat = first + lo + (int)e;
+                t.need = completed[e];
+                const int product = (int)plan->products.size();
+                plan->products.push_back(t);
+                const size_t begin = plan->tasks.size();
+                each_tile(ceil_div(t.m, side), ceil_div(t.width, side), t.phase < MUON_UPDATE,
+                          [&](int i, int j) { plan->tasks.push_back(MuonTask{product, (short)i, (short)j}); });
+                completed[e] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(ctas * MUON_EPI_WARPS);
+            }
+        }
     }
 }
 
@@ -223,6 +279,7 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
         m.ldx = (int)round_up(m.n, 64);
         m.lde = (int)round_up(m.m, 64);
         m.precise = m.m <= PRECISE_SIDE;
+        m.symmetric = in_twos(m, c->cfg.steps) ? 3 : 2;
         m.tensor = t;
         // X's elements are of order one once its singular values are: then neither hi nor lo leaves the normal range of fp16
         m.S = (float)std::exp2(std::floor(0.5 * std::log2((double)m.n)));
@@ -339,10 +396,10 @@ demo_status build(demo_muon_ctx *c)
     std::memset(maps.data(), 0, maps.size() * sizeof(CUtensorMap));
     for (MuonMat &m : plan.mats) {
         CUtensorMap *p = &maps[(size_t)m.maps];
-        for (int x = 0; x < 2; ++x)
-            ok = ok && encode_maps(encode, p + MUON_MAP_X0 + x, m.xhi[x], m.n, m.m, m.ldx) && encode_maps(encode, p + MUON_MAP_XLO0 + x, m.xlo[x], m.n, m.m, m.ldx);
-        ok = ok && encode_maps(encode, p + MUON_MAP_E, m.ehi, m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_ELO, m.elo, m.m, m.m, m.lde) &&
-             encode_maps(encode, p + MUON_MAP_F, m.fhi, m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_FLO, m.flo, m.m, m.m, m.lde);
+        for (int k = 0; k < 2; ++k)
+            ok = ok && encode_maps(encode, p + MUON_MAP_X + k, m.xhi[k], m.n, m.m, m.ldx) && encode_maps(encode, p + MUON_MAP_XLO + k, m.xlo[k], m.n, m.m, m.ldx);
+        for (int k = 0; k < m.symmetric; ++k)
+            ok = ok && encode_maps(encode, p + MUON_MAP_E + k, m.ehi[k], m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_ELO + k, m.elo[k], m.m, m.m, m.lde);
     }
     if (!ok) return DEMO_ERR_CUDA;
     ok = cudaMemcpy(c->d_mats, plan.mats.data(), T * sizeof(MuonMat), cudaMemcpyHostToDevice) == cudaSuccess &&
