@@ -337,6 +337,13 @@ __device__ __forceinline__ void arrive_release_cluster(uint32_t bar)
 constexpr long long TASK_WAIT_CYCLES = 20000000000LL;  // ~10 s: what is waited for may be other workers' tasks, long ones for large matrices
 
 __device__ __forceinline__ bool wait_local(uint32_t bar, unsigned parity) { return mbar_wait_bounded(bar, parity, TASK_WAIT_CYCLES); }
+// Whether a phase is complete, without the pause that a try_wait may take (4 us).
+__device__ __forceinline__ bool mbar_test(uint32_t bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
 // as wait_local, seeing what another CTA of the cluster did before its arrival
 __device__ __forceinline__ bool wait_cluster(uint32_t bar, unsigned parity)
 {
@@ -437,6 +444,7 @@ struct BlockAt {
     float *dst;         // and of the result's
     uint32_t tmem;
     int r0, j0, lane;
+    float column;       // POLY, MUL: the right factor's diagonal at column j0 + lane
     float *st;          // the warp's 4 KB of shared memory
 };
 
@@ -483,12 +491,6 @@ __device__ __forceinline__ void load_block(const float *p, float4 (&x)[8])
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(p + k * 128));
 }
-// 32 elements of a vector, the same for all lanes
-__device__ __forceinline__ void load_vector(const float *p, float4 (&x)[8])
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(p) + k);
-}
 __device__ __forceinline__ void store_block(float *p, const float (&v)[32])
 {
 #pragma unroll
@@ -516,23 +518,21 @@ __device__ __forceinline__ void block_gram(const MuonArgs &a, const MuonProduct 
 #pragma unroll
     for (int k = 0; k < 32; ++k) v[k] *= t.scale;
     if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, take_own(v, b.lane) * MUON_EF_INV);
-    store_block(b.dst, v);
     write_halves(a, t, b, turn, v);
+    store_block(b.dst, v);
 }
 
 // B = a + b A + c A^2
 __device__ __forceinline__ void block_poly(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&e)[8], float di)
 {
     float v[32];
-    float4 dj[8];
-    load_vector(t.vec + b.j0, dj);
     tmem_ld32(b.tmem, v);
     if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, a.a + fmaf(a.b, di, a.c * fmaf(di, di, take_own(v, b.lane) * (MUON_EF_INV * MUON_EF_INV))));
     const float base = fmaf(a.c, di, a.b), scale = a.c * MUON_EF_INV;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(fmaf(a.c, part(dj, k), base), part(e, k), scale * v[k]);  // (E's own diagonal is zero)
-    if (t.dst) store_block(b.dst, v);
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(fmaf(a.c, __shfl_sync(0xffffffffu, b.column, k), base), part(e, k), scale * v[k]);  // (E's own diagonal is zero)
     write_halves(a, t, b, turn, v);
+    if (t.dst) store_block(b.dst, v);
 }
 
 // P Q, of matrices that commute
@@ -542,14 +542,13 @@ __device__ __forceinline__ void block_mul(const MuonArgs &a, const MuonProduct &
     float4 f[8];
     load_block(b.src2, f);
     tmem_ld32(b.tmem, v);
-    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, fmaf(di, __ldcg(t.vec2 + b.r0 + b.lane), take_own(v, b.lane) * (MUON_EF_INV * MUON_EF_INV)));
+    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, fmaf(di, b.column, take_own(v, b.lane) * (MUON_EF_INV * MUON_EF_INV)));
 #pragma unroll
     for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(f, k), v[k] * MUON_EF_INV);
-    load_vector(t.vec2 + b.j0, f);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(part(e, k), part(f, k), v[k]);
-    if (t.dst) store_block(b.dst, v);
+    for (int k = 0; k < 32; ++k) v[k] = fmaf(part(e, k), __shfl_sync(0xffffffffu, b.column, k), v[k]);
     write_halves(a, t, b, turn, v);
+    if (t.dst) store_block(b.dst, v);
 }
 
 // X <- B X
@@ -559,8 +558,8 @@ __device__ __forceinline__ void block_update(const MuonArgs &a, const MuonProduc
     tmem_ld32(b.tmem, v);
 #pragma unroll
     for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV);
-    store_block(b.dst, v);
     write_halves(a, t, b, turn, v);
+    store_block(b.dst, v);
 }
 
 // The same, the last time: to the caller's tensor.
@@ -736,6 +735,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                     ok = false;
                     break;
                 }
+                fence_proxy_async_all();  // what they wrote is read by this CTA's copies
                 if (CG == 2 && rank == 0) {
                     ok = wait_cluster(q_empty + 8 * slot, turn ^ 1);
                     if (!ok) break;
@@ -790,11 +790,10 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 arrive(r_empty + 8 * slot);
                 next_slot();
                 if (end) break;
-                fence_proxy_async_all();
                 int left_steps = steps * parts;
-                for (int part = 0; ok && part < parts; ++part) {  // hi hi, hi lo, lo hi
-                    const char *ml = part == 2 ? left_lo : left, *mr = part == 1 ? right_lo : right;
-                    for (int k = 0; k < steps; ++k) {
+                for (int k = 0; k < steps; ++k)
+                    for (int part = 0; ok && part < parts; ++part) {  // hi, lo
+                        const char *ml = part ? left_lo : left, *mr = part ? right_lo : right;
                         if (left_steps-- == min(steps * parts, NEAR_STEPS)) arrive(near_end);
                         ok = wait_local(empty + 8 * stage, phase ^ 1);
                         if (!ok) break;
@@ -811,7 +810,6 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                         ++used;
                         if (++stage == STAGES) stage = 0, phase ^= 1;
                     }
-                }
                 if (!ok) break;
             }
             // before the CTA ends, every stage has been read (after a failure: waited for, as long as a wait lasts)
@@ -841,18 +839,14 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 tc_after();
                 const uint32_t d = tmem + acc * 256;
                 uint32_t accumulate = 0;
-                for (int part = 0; ok && part < parts; ++part)
-                    for (int k = 0; k < steps; ++k) {
-                        // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row.  MN-major: blocks of 64
-                        // columns 8192 bytes apart, groups of 8 rows of K 1024.
-                        const bool a_mn = 64 * k < left_rows, b_mn = 64 * k < right_rows;
-                        const uint32_t idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
-                        const uint32_t A = base + stage * STAGE;
-                        uint64_t da = operand_desc(A, a_mn ? 8192 : 16, 1024), db = operand_desc(A + OPERAND, b_mn ? 8192 : 16, 1024);
-                        const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
-                        ok = wait_local(full + 8 * stage, phase);
-                        if (!ok) break;
-                        tc_after();
+                for (int k = 0; k < steps; ++k) {
+                    // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row.  MN-major: blocks of 64
+                    // columns 8192 bytes apart, groups of 8 rows of K 1024.
+                    const bool a_mn = 64 * k < left_rows, b_mn = 64 * k < right_rows;
+                    const uint32_t idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+                    const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
+                    auto multiply = [&](int sa, int sb) {
+                        uint64_t da = operand_desc(base + sa * STAGE, a_mn ? 8192 : 16, 1024), db = operand_desc(base + sb * STAGE + OPERAND, b_mn ? 8192 : 16, 1024);
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {
                             mma_f16<CG>(d, da, db, idesc, accumulate);
@@ -860,9 +854,26 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                             da += a_step;
                             db += b_step;
                         }
+                    };
+                    ok = wait_local(full + 8 * stage, phase);
+                    if (!ok) break;
+                    tc_after();
+                    const int hi = stage;
+                    multiply(hi, hi);
+                    if (++stage == STAGES) stage = 0, phase ^= 1;
+                    if (parts > 1) {  // the next stage holds the lo parts
+                        ok = wait_local(full + 8 * stage, phase);
+                        if (!ok) break;
+                        tc_after();
+                        multiply(hi, stage);
+                        multiply(stage, hi);
+                        mma_commit<CG>(empty + 8 * hi);
                         mma_commit<CG>(empty + 8 * stage);
                         if (++stage == STAGES) stage = 0, phase ^= 1;
+                    } else {
+                        mma_commit<CG>(empty + 8 * hi);
                     }
+                }
                 if (!ok) break;
                 mma_commit<CG>(t_full + 8 * acc);
             }
@@ -892,7 +903,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             __syncwarp();
         };
         for (int n_done = 0;; ++n_done) {
-            if (!__all_sync(0xffffffffu, mbar_try_wait(r_full + 8 * slot, turn))) tell();
+            if (!__all_sync(0xffffffffu, mbar_test(r_full + 8 * slot, turn))) tell();
             ok = wait_local(r_full + 8 * slot, turn);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -906,8 +917,9 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             const int acc = n_done & 1;
             const size_t at = ((size_t)(r0 / 32) * t.blocks + first / 32) * 1024 + lane * 4;
             float4 x[8], next[8];
-            float row = 0.f;
+            float row = 0.f, next_column = 0.f;
             if (blocks > 0 && t.phase != MUON_GRAM) {
+                if (t.phase <= MUON_MUL) next_column = __ldcg(t.vec2 + first + lane);
                 load_block(t.src + at, next);
                 row = __ldcg(t.vec + r0 + lane);
             }
@@ -928,8 +940,12 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 for (int b = 0; b < blocks; ++b) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) x[k] = next[k];
-                    if (t.phase != MUON_GRAM && b + 1 < blocks) load_block(t.src + at + (b + 1) * 1024, next);
-                    use(BlockAt{t.src2 + at + b * 1024, t.dst + at + b * 1024, tmem + acc * 256 + half * (TILE / 2) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, st});
+                    const float column = next_column;
+                    if (t.phase != MUON_GRAM && b + 1 < blocks) {
+                        load_block(t.src + at + (b + 1) * 1024, next);
+                        if (t.phase <= MUON_MUL) next_column = __ldcg(t.vec2 + first + 32 * (b + 1) + lane);
+                    }
+                    use(BlockAt{t.src2 + at + b * 1024, t.dst + at + b * 1024, tmem + acc * 256 + half * (TILE / 2) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, column, st});
                 }
             };
             if (t.phase == MUON_GRAM)
@@ -971,13 +987,12 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
 }
 
 template <int CG>
-cudaError_t launch_products(const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, DemoLaunch &dev, cudaStream_t stream)
+cudaError_t launch_products(const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
 {
     const void *kernel = reinterpret_cast<const void *>(muon_products_kernel<CG>);
     cudaError_t err = demo_allow_smem(dev, kernel);
     if (err != cudaSuccess) return err;
-    const int most = dev.sm_count / CG;
-    const int grid = (n_tasks < most ? n_tasks : most) * CG;
+    const int grid = workers * CG;
     MuonArgs args = a;
     void *params[] = {&args, &products, &tasks, &n_tasks};
     cudaLaunchAttribute attr[2];
@@ -1012,7 +1027,7 @@ cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_til
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_pack_kernel), n_tiles, NORM_THREADS, 0, stream, params);
 }
 
-cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, DemoLaunch &dev, cudaStream_t stream)
+cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
 {
-    return pair ? launch_products<2>(a, products, tasks, n_tasks, dev, stream) : launch_products<1>(a, products, tasks, n_tasks, dev, stream);
+    return pair ? launch_products<2>(a, products, tasks, n_tasks, workers, dev, stream) : launch_products<1>(a, products, tasks, n_tasks, workers, dev, stream);
 }

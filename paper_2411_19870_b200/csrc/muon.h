@@ -69,7 +69,7 @@ struct alignas(16) MuonProduct {  // what the tasks of one product of one matrix
     int phase, mat;
     unsigned need;
     int steps;               // of K = 64
-    int parts;               // 1: hi hi; 3: hi lo and lo hi, too
+    int parts;               // 1: the product of the hi parts; 2: hi lo and lo hi, too
     int left, right, out;    // tensor maps of the operands and of the result
     int left_lo, right_lo, out_lo;
     int blocks;              // of x32 / e32 in a row of them
@@ -113,5 +113,5 @@ cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n
 // X = S u / (||u|| + eps), as hi + lo; clears the counters of the matrices [first_mat, first_mat + n_mats) and the next task.
 cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, DemoLaunch &dev, cudaStream_t stream);
 // All products.  pair: tiles of 256 x 256 by clusters of two CTAs; otherwise 128 x 128 by one.
-cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, DemoLaunch &dev, cudaStream_t stream);
+cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
 constexpr int MUON_EPI_WARPS = 8;  // completions of a task: one for each of them in every CTA

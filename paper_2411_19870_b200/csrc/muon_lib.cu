@@ -23,7 +23,7 @@ struct Group {
     long long pack_tiles;  // first of its list
     int n_pack;
     long long tasks;
-    int n_tasks;
+    int n_tasks, workers;
 };
 
 // Pointer arrays of an entry point: device table and mirror, uploaded when they change.
@@ -168,7 +168,7 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
         const bool wide = phase >= MUON_UPDATE;
         t.phase = phase;
         t.steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
-        t.parts = m.precise ? 3 : 1;
+        t.parts = m.precise ? 2 : 1;
         t.m = m.m;
         t.width = wide ? m.n : m.m;
         t.blocks = (wide ? m.ldx : m.lde) / 32;
@@ -232,8 +232,9 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
 
 // The products of the matrices mats[0 .. n), `first` the index of the first.  Matrices go through the iterations in cohorts, product by product,
 // every product matrix by matrix: with two rounds of the workers' tasks in a cohort's symmetric products, a matrix's next product starts when its last
-// is done, and the X of a cohort of small matrices stays in L2.
-void add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bool pair, Plan *plan)
+// is done, and the X of a cohort of small matrices stays in L2.  Returns how many workers the tasks keep busy: more would take turns, and every one of
+// them would come with cold instruction caches (one 256 x 512: 70 workers 155 us, 8 XXX).
+int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bool pair, Plan *plan)
 {
     const int side = pair ? 256 : 128, ctas = pair ? 2 : 1, workers = std::max(1, c->launch.sm_count / ctas);
     auto symmetric = [&](const MuonMat &m) { const long long k = ceil_div(m.m, side); return k * (k + 1) / 2; };
@@ -241,6 +242,7 @@ void add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bo
     for (int e = 0; e < n; ++e) total += symmetric(mats[e]);
     const long long cohorts = std::max(1LL, total / (2LL * workers));
     long long before = 0;
+    size_t most = 1;
     for (int lo = 0, hi = 0; lo < n; lo = hi) {
         const long long which = before * cohorts / total;
         for (; hi < n && (hi == lo || before * cohorts / total == which); ++hi) before += symmetric(mats[hi]);
@@ -249,6 +251,7 @@ void add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bo
         std::vector<unsigned> completed(lists.size(), 0u);
         for (size_t k = 0, more = 1; more; ++k) {
             more = 0;
+            const size_t step = plan->tasks.size();
             for (size_t e = 0; e < lists.size(); ++e) {
                 if (k >= lists[e].size()) continue;
                 more = 1;
@@ -262,8 +265,10 @@ void add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bo
                           [&](int i, int j) { plan->tasks.push_back(MuonTask{product, (short)i, (short)j}); });
                 completed[e] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(ctas * MUON_EPI_WARPS);
             }
+            most = std::max(most, plan->tasks.size() - step);
         }
     }
+    return (int)std::min(most, (size_t)workers);
 }
 
 demo_status make_plan(demo_muon_ctx *c, Plan *plan)
@@ -330,7 +335,7 @@ demo_status make_tasks(demo_muon_ctx *c, Plan *plan)
 {
     for (Group &g : c->groups) {
         g.tasks = (long long)plan->tasks.size();
-        add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.pair, plan);
+        g.workers = add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.pair, plan);
         g.n_tasks = (int)((long long)plan->tasks.size() - g.tasks);
         if (plan->tasks.size() > (size_t)(1LL << 30)) return DEMO_ERR_UNSUPPORTED;
     }
@@ -461,7 +466,7 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     for (const Group &grp : c->groups) {
         if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, stream);
         if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, c->launch, stream);
-        if (err == cudaSuccess) err = muon_launch_products(grp.pair, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, c->launch, stream);
+        if (err == cudaSuccess) err = muon_launch_products(grp.pair, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, stream);
         c->launches += 3;
     }
     if (err != cudaSuccess) {
