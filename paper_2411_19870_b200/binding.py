@@ -172,7 +172,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.demo_adamw_free.restype = None
     # addresses of the per-step calls, for csrc/calls.cpp
     lib.entry_points = {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value
-                        for n in ("demo_compress", "demo_decode_apply", "demo_decode_signs", "demo_apply_signs")}
+                        for n in ("demo_compress", "demo_decode_apply", "demo_decode_signs", "demo_apply_signs", "demo_orthogonalize",
+                                  "demo_muon_step", "demo_muon_decode_apply", "demo_adamw_step")}
     if path is None:
         _lib = lib
     return lib
@@ -538,34 +539,47 @@ class MuonTransform:
             self._ctx = ctypes.c_void_p()
             raise DemoError(st, "demo_muon_init")
         self._grad = torch.bfloat16 if grad_dtype == DEMO_BF16 else torch.float32
+        self._calls, self._fn = load_calls(), self.lib.entry_points
+        self._layouts = {d: self._calls.layouts(d, device, self.shapes) for d in _DTYPES}
 
+    # As in DemoTransform: csrc/calls.cpp answers None for what does not fit, and for subclasses of Tensor.
     def orthogonalize(self, inputs, outputs, stream=None) -> None:
         """``outputs[t] = O(inputs[t])``; inputs of one type, outputs of one type, each fp32 or bf16."""
         inputs, outputs = list(inputs), list(outputs)
         for what, ts in (("inputs", inputs), ("outputs", outputs)):
             if not ts or ts[0].dtype not in _DTYPES:
                 raise ValueError("%s: expected fp32 or bf16 tensors" % what)
-        st = self.lib.demo_orthogonalize(self._ctx, _checked(inputs, self.shapes, inputs[0].dtype, self.device, "inputs"),
-                                         _DTYPES[inputs[0].dtype],
-                                         _checked(outputs, self.shapes, outputs[0].dtype, self.device, "outputs"),
-                                         _DTYPES[outputs[0].dtype], DemoTransform._stream(stream))
+        a, b = inputs[0].dtype, outputs[0].dtype
+        st = self._calls.orthogonalize(self._fn["demo_orthogonalize"], self._ctx.value or 0, self._layouts[a], inputs, _DTYPES[a],
+                                       self._layouts[b], outputs, _DTYPES[b], DemoTransform._raw_stream(stream))
+        if st is None:
+            st = self.lib.demo_orthogonalize(self._ctx, _checked(inputs, self.shapes, a, self.device, "inputs"), _DTYPES[a],
+                                             _checked(outputs, self.shapes, b, self.device, "outputs"), _DTYPES[b],
+                                             DemoTransform._stream(stream))
         if st != 0:
             raise DemoError(st, "demo_orthogonalize")
 
     def step(self, grads, momentum, params, stream=None) -> None:
-        st = self.lib.demo_muon_step(self._ctx, _checked(grads, self.shapes, self._grad, self.device, "grads"),
-                                     _checked(momentum, self.shapes, torch.float32, self.device, "momentum"),
-                                     _checked(params, self.shapes, torch.float32, self.device, "params"), DemoTransform._stream(stream))
+        f32 = self._layouts[torch.float32]
+        st = self._calls.muon_step(self._fn["demo_muon_step"], self._ctx.value or 0, self._layouts[self._grad], f32, grads, momentum, params,
+                                   DemoTransform._raw_stream(stream))
+        if st is None:
+            st = self.lib.demo_muon_step(self._ctx, _checked(grads, self.shapes, self._grad, self.device, "grads"),
+                                         _checked(momentum, self.shapes, torch.float32, self.device, "momentum"),
+                                         _checked(params, self.shapes, torch.float32, self.device, "params"), DemoTransform._stream(stream))
         if st != 0:
             raise DemoError(st, "demo_muon_step")
 
     def decode_apply(self, demo: DemoTransform, payloads, params, stream=None) -> None:
         """``demo.decode_apply`` with orthogonalised updates of its matrices, which are those of this context; ``params``: all of ``demo``'s."""
-        payloads = list(payloads)
-        demo._check_payloads(payloads)
-        st = self.lib.demo_muon_decode_apply(self._ctx, demo._ctx, _ptr_array(_tensor_ptrs(payloads)), len(payloads),
-                                             _checked(params, demo.shapes, torch.float32, self.device, "params"),
-                                             DemoTransform._stream(stream))
+        st = self._calls.muon_decode(self._fn["demo_muon_decode_apply"], self._ctx.value or 0, demo._ctx.value or 0, demo._payload_ok, payloads,
+                                     demo._f32[1], params, DemoTransform._raw_stream(stream))
+        if st is None:
+            payloads = list(payloads)
+            demo._check_payloads(payloads)
+            st = self.lib.demo_muon_decode_apply(self._ctx, demo._ctx, _ptr_array(_tensor_ptrs(payloads)), len(payloads),
+                                                 _checked(params, demo.shapes, torch.float32, self.device, "params"),
+                                                 DemoTransform._stream(stream))
         if st != 0:
             raise DemoError(st, "demo_muon_decode_apply")
 
@@ -613,15 +627,22 @@ class AdamwTransform:
             self._ctx = ctypes.c_void_p()
             raise DemoError(st, "demo_adamw_init")
         self._grad = torch.bfloat16 if grad_dtype == DEMO_BF16 else torch.float32
+        self._calls, self._fn = load_calls(), self.lib.entry_points
+        self._layouts = {d: self._calls.layouts(d, device, self.shapes) for d in _DTYPES}
+        self._count = self._calls.layouts(torch.int64, device, [(1,)])
 
     def step(self, grads, exp_avg, exp_avg_sq, params, step: torch.Tensor, stream=None) -> None:
         """``step``: int64 tensor of one element on the device, the number of steps made so far; this call adds one."""
-        if step.dtype != torch.int64 or step.numel() != 1 or not step.is_cuda or step.device.index != self.device:
-            raise ValueError("step: need an int64 tensor of one element on cuda:%d" % self.device)
-        lists = [_checked(t, self.shapes, d, self.device, w) for t, d, w in (
-            (grads, self._grad, "grads"), (exp_avg, torch.float32, "exp_avg"), (exp_avg_sq, torch.float32, "exp_avg_sq"),
-            (params, torch.float32, "params"))]
-        st = self.lib.demo_adamw_step(self._ctx, *lists, ctypes.c_void_p(step.data_ptr()), DemoTransform._stream(stream))
+        f32 = self._layouts[torch.float32]
+        st = self._calls.adamw_step(self._fn["demo_adamw_step"], self._ctx.value or 0, self._layouts[self._grad], f32, grads, exp_avg, exp_avg_sq,
+                                    params, self._count, (step,), DemoTransform._raw_stream(stream))
+        if st is None:
+            if step.dtype != torch.int64 or step.numel() != 1 or not step.is_cuda or step.device.index != self.device:
+                raise ValueError("step: need an int64 tensor of one element on cuda:%d" % self.device)
+            lists = [_checked(t, self.shapes, d, self.device, w) for t, d, w in (
+                (grads, self._grad, "grads"), (exp_avg, torch.float32, "exp_avg"), (exp_avg_sq, torch.float32, "exp_avg_sq"),
+                (params, torch.float32, "params"))]
+            st = self.lib.demo_adamw_step(self._ctx, *lists, ctypes.c_void_p(step.data_ptr()), DemoTransform._stream(stream))
         if st != 0:
             raise DemoError(st, "demo_adamw_step")
 

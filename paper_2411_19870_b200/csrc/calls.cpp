@@ -6,7 +6,7 @@
 // the checks in Python, ctypes' conversion of the arguments, the device and stream queries).  Without it -> with it, tensors where the call
 // before had them / tensors elsewhere, whose pointers the library copies to the device: compress of one matrix 5.6 -> 3.0 / 15.5 -> 9.6 us,
 // of 50 matrices and 12 vectors (two launches) 16.3 -> 7.1 / 93 -> 20, decode of the same set 12.2 -> 6.4 / 48 -> 9.8, of 64 payloads
-// 28.4 -> 8.1 / 38.4 -> 11.6.
+// 28.4 -> 8.1 / 38.4 -> 11.6; AdamW of five vectors 21.6 -> XXX.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -249,11 +249,129 @@ PyObject *apply_signs(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// The pointers of a list of tensors proper that fit `capsule`'s layouts.
+Found gather(PyObject *capsule, PyObject *tensors, c10::SmallVectorImpl<void *> &out)
+{
+    const Layouts *l = static_cast<const Layouts *>(PyCapsule_GetPointer(capsule, LAYOUTS));
+    if (!l) return Found::error;
+    if (!PyList_Check(tensors) && !PyTuple_Check(tensors)) return Found::no;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(tensors);
+    if (l->size() != n) return Found::no;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject *t = PySequence_Fast_GET_ITEM(tensors, i);
+        if (!THPVariable_CheckExact(t) || !l->fits(THPVariable_Unpack(t), i)) return Found::no;
+        out.push_back(THPVariable_Unpack(t).data_ptr());
+    }
+    return Found::yes;
+}
+using Pointers = c10::SmallVector<void *, 64>;
+
+using OrthogonalizeFn = int (*)(void *, void **, std::int32_t, void **, std::int32_t, void *);
+using MuonStepFn = int (*)(void *, void **, void **, void **, void *);
+using MuonDecodeFn = int (*)(void *, void *, void **, std::int32_t, void **, void *);
+using AdamwStepFn = int (*)(void *, void **, void **, void **, void **, void *, void *);
+
+// orthogonalize(function, context, layouts of inputs, inputs, their type, layouts of outputs, outputs, their type, stream or None)
+PyObject *orthogonalize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "orthogonalize: 9 arguments");
+    void *fn = PyLong_AsVoidPtr(a[0]), *ctx = PyLong_AsVoidPtr(a[1]), *stream = nullptr;
+    const long in_type = PyLong_AsLong(a[4]), out_type = PyLong_AsLong(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    Pointers in, out;
+    Found f = gather(a[2], a[3], in);
+    if (f == Found::yes) f = gather(a[5], a[6], out);
+    if (f != Found::yes) return slow(f);
+    if (!stream_of(a[8], &stream)) return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = reinterpret_cast<OrthogonalizeFn>(fn)(ctx, in.data(), (std::int32_t)in_type, out.data(), (std::int32_t)out_type, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// muon_step(function, context, layouts of grads, of momentum and params, grads, momentum, params, stream or None)
+PyObject *muon_step(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "muon_step: 8 arguments");
+    void *fn = PyLong_AsVoidPtr(a[0]), *ctx = PyLong_AsVoidPtr(a[1]), *stream = nullptr;
+    if (PyErr_Occurred()) return nullptr;
+    Pointers g, m, x;
+    Found f = gather(a[2], a[4], g);
+    if (f == Found::yes) f = gather(a[3], a[5], m);
+    if (f == Found::yes) f = gather(a[3], a[6], x);
+    if (f != Found::yes) return slow(f);
+    if (!stream_of(a[7], &stream)) return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = reinterpret_cast<MuonStepFn>(fn)(ctx, g.data(), m.data(), x.data(), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// muon_decode(function, context, context that made the payloads, its known payloads, payloads, layouts of params, params, stream or None)
+PyObject *muon_decode(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "muon_decode: 8 arguments");
+    void *fn = PyLong_AsVoidPtr(a[0]), *ctx = PyLong_AsVoidPtr(a[1]), *demo = PyLong_AsVoidPtr(a[2]), *stream = nullptr;
+    if (PyErr_Occurred()) return nullptr;
+    if (!PyList_Check(a[4]) && !PyTuple_Check(a[4])) Py_RETURN_NONE;
+    Pointers p, x;
+    Found f = gather(a[5], a[6], x);
+    const Layouts *l = f == Found::yes ? static_cast<const Layouts *>(PyCapsule_GetPointer(a[5], LAYOUTS)) : nullptr;
+    for (Py_ssize_t i = 0; f == Found::yes && i < PySequence_Fast_GET_SIZE(a[4]); ++i) {
+        std::uintptr_t ptr;
+        f = payload_known(a[3], PySequence_Fast_GET_ITEM(a[4], i), l, &ptr);
+        if (f == Found::yes) p.push_back(reinterpret_cast<void *>(ptr));
+    }
+    if (f != Found::yes) return slow(f);
+    if (!stream_of(a[7], &stream)) return nullptr;
+    const std::int32_t count = (std::int32_t)p.size();
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = reinterpret_cast<MuonDecodeFn>(fn)(ctx, demo, p.data(), count, x.data(), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// adamw_step(function, context, layouts of grads, of the fp32 lists, grads, exp_avg, exp_avg_sq, params, layouts of the count, [count], stream or None)
+PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 11) return PyErr_Format(PyExc_TypeError, "adamw_step: 11 arguments");
+    void *fn = PyLong_AsVoidPtr(a[0]), *ctx = PyLong_AsVoidPtr(a[1]), *stream = nullptr;
+    if (PyErr_Occurred()) return nullptr;
+    Pointers g, m, v, x, count;
+    Found f = gather(a[2], a[4], g);
+    if (f == Found::yes) f = gather(a[3], a[5], m);
+    if (f == Found::yes) f = gather(a[3], a[6], v);
+    if (f == Found::yes) f = gather(a[3], a[7], x);
+    if (f == Found::yes) f = gather(a[8], a[9], count);
+    if (f != Found::yes) return slow(f);
+    if (!stream_of(a[10], &stream)) return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = reinterpret_cast<AdamwStepFn>(fn)(ctx, g.data(), m.data(), v.data(), x.data(), count[0], stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"layouts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(make_layouts)), METH_FASTCALL, nullptr},
     {"compress", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(compress)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode)), METH_FASTCALL, nullptr},
     {"apply_signs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(apply_signs)), METH_FASTCALL, nullptr},
+    {"orthogonalize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(orthogonalize)), METH_FASTCALL, nullptr},
+    {"muon_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(muon_step)), METH_FASTCALL, nullptr},
+    {"muon_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(muon_decode)), METH_FASTCALL, nullptr},
+    {"adamw_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(adamw_step)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
