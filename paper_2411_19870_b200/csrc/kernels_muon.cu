@@ -250,11 +250,9 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
 constexpr int EPI_WARPS = MUON_EPI_WARPS;
 constexpr int SCHEDULER = EPI_WARPS + 2;       // its warp
 constexpr int THREADS = 96 + 32 * EPI_WARPS;  // loading warp, MMA warp, epilogue, scheduler
-constexpr int OPERAND = 16384;                // 128 rows (K-major) or 64 x 128 (MN-major) fp16 elements of one step of K = 64
-constexpr int STAGE = 2 * OPERAND;
-constexpr int STAGES = 6;
+constexpr int RING_BYTES = 6 * 32768;         // of operands: steps of K = 64, both operands of a CTA
 constexpr int TMEM_COLS = 512;
-constexpr int SMEM = STAGES * STAGE + EPI_WARPS * 4096 + 1024;
+constexpr int SMEM = RING_BYTES + EPI_WARPS * 4096 + 1024;
 
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -282,50 +280,40 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, uint32_t lbo, u
            (uint64_t)2 << 61;
 }
 
-template <int CG>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    if constexpr (CG == 1)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
-                     "r"(idesc), "r"(accumulate)
-                     : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
-                     "r"(idesc), "r"(accumulate)
-                     : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                 "r"(accumulate)
+                 : "memory");
 }
-// Arrives at `bar` (of both CTAs of a pair) once the MMAs issued so far are done.
-template <int CG>
+// Arrives at `bar` of both CTAs of the pair once the MMAs issued so far are done.
 __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
-    if constexpr (CG == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// One operand of a step: 128 rows of 64 elements (K-major), or, column by column, two blocks of 64 rows of K (MN-major).  A pair's loads are
-// counted by the barrier of its first CTA.
-template <int CG>
-__device__ __forceinline__ void load_rows(uint32_t dst, const void *map, int x, int y, uint32_t bar)
+// One operand of a step: rows of 64 elements (K-major), or, column by column, blocks of 64 rows of K (MN-major; two of them side by side come
+// as a third dimension).  The loads of both CTAs are counted by the barrier of the first.
+__device__ __forceinline__ void load_2d(uint32_t dst, const void *map, int x, int y, uint32_t bar)
 {
-    if constexpr (CG == 1)
-        tma_load_2d(dst, map, x, y, bar);
-    else
-        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
-                     "r"(x), "r"(y), "r"(bar)
-                     : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x),
+                 "r"(y), "r"(bar)
+                 : "memory");
 }
-template <int CG>
-__device__ __forceinline__ void load_columns(uint32_t dst, const void *map, int x, int y, uint32_t bar)
+__device__ __forceinline__ void load_3d(uint32_t dst, const void *map, int x, int y, uint32_t bar)
 {
-    if constexpr (CG == 1)
-        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(0),
-                     "r"(y), "r"(x / 64), "r"(bar)
-                     : "memory");
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(0),
+                 "r"(y), "r"(x / 64), "r"(bar)
+                 : "memory");
+}
+template <int ROWS>
+__device__ __forceinline__ void load_operand(uint32_t dst, const char *map, bool columns, int at, int k, uint32_t bar)
+{
+    if (!columns)
+        load_2d(dst, map, k, at, bar);
+    else if (ROWS == 64)
+        load_2d(dst, map, at, k, bar);
     else
-        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
-                     "r"(0), "r"(y), "r"(x / 64), "r"(bar)
-                     : "memory");
+        load_3d(dst, map + MUON_MAP_MN * MUON_MAP_BYTES, at, k, bar);
 }
 // (release at the scope of the CTA even where the barrier is another CTA's: one of the cluster's would wait for this warp's stores to memory)
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
@@ -337,6 +325,17 @@ __device__ __forceinline__ void arrive_release_cluster(uint32_t bar)
 constexpr long long TASK_WAIT_CYCLES = 20000000000LL;  // ~10 s: what is waited for may be other workers' tasks, long ones for large matrices
 
 __device__ __forceinline__ bool wait_local(uint32_t bar, unsigned parity) { return mbar_wait_bounded(bar, parity, TASK_WAIT_CYCLES); }
+// One lane of a warp that runs converged.  The loading and the MMA warp loop with all their lanes and leave only the instructions themselves to
+// one: operands formed in divergent code cost each MMA and each copy 100 to 200 cycles on their way to uniform registers (a step of a 256 tile:
+// 581 cycles instead of XXX, of which the products take 512).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ bool all_of(bool ok) { return __all_sync(0xffffffffu, ok); }
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 // Whether a phase is complete, without the pause that a try_wait may take (4 us).
 __device__ __forceinline__ bool mbar_test(uint32_t bar, unsigned parity)
 {
@@ -629,18 +628,20 @@ struct alignas(16) RingEntry {
     int i, j, end, pad;
 };
 
-// All products of all iterations, by persistent workers (CTAs; CG = 2: pairs).  Tasks are drawn in the list's order from one counter, so
+// All products of all iterations, by persistent workers, pairs of CTAs.  Tasks are drawn in the list's order from one counter, so
 // whatever a task waits for is done already or in the hands of a worker that runs: no worker has to be resident for another to go on.
 // One warp loads, one issues the MMAs, eight read accumulators back: two of them, so that the products of a task run beside the epilogue
 // of the one before.  A fourth kind of warp schedules: that of a worker's first CTA draws the tasks and waits until they may start, and in
 // both CTAs it puts what the others need to know of one into a ring, up to four ahead (by the loading warp itself: its look-ups and waits,
 // 3500 cycles a task, leave the tensor core without data).
 // Symmetric matrices exist above the diagonal only: left of it a panel's operand is loaded from the rows above, as its transpose.
-template <int CG>
+// A worker's tile is TILE x TILE: 256, of which each CTA's tensor memory holds half the rows, or 128, for small matrices: of its 64 rows a CTA
+// then holds the left 64 columns in lanes 0 .. 63 and the right ones in lanes 64 .. 127.
+template <int TILE>
 __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
 {
     const StreamOrder order(1);
-    constexpr int TILE = 128 * CG;  // of both sides
+    constexpr int ROWS = TILE / 2, OPERAND = ROWS * 128, STAGE = 2 * OPERAND, STAGES = RING_BYTES / STAGE;
     constexpr int RING = 4, NEAR_STEPS = 8;
     extern __shared__ unsigned char raw[];
     __shared__ unsigned long long bars[2 * STAGES + 4 + 4 * RING + 2];
@@ -649,7 +650,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
     __shared__ uint32_t tmem_slot;
     const uint32_t raw_s = smem_u32(raw), base = (raw_s + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    const uint32_t rank = cluster_rank();
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, t_full = empty + 8 * STAGES, t_empty = t_full + 16, r_full = t_empty + 16,
                    r_empty = r_full + 8 * RING, q_full = r_empty + 8 * RING, q_empty = q_full + 8 * RING, near_end = q_empty + 8 * RING, drained = near_end + 8;
     if (threadIdx.x == 0) {
@@ -659,7 +660,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(t_full + 8 * s, 1);
-            mbar_init(t_empty + 8 * s, CG * EPI_WARPS);
+            mbar_init(t_empty + 8 * s, 2 * EPI_WARPS);
         }
         for (int s = 0; s < RING; ++s) {
             mbar_init(r_full + 8 * s, 1);
@@ -674,17 +675,12 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
     }
     order.begin();
     if (warp == 0) {
-        if constexpr (CG == 1) {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(TMEM_COLS) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(TMEM_COLS) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        }
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();
+    cluster_sync();
     tc_after();
     const uint32_t tmem = tmem_slot;
     bool ok = true;
@@ -724,7 +720,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                         const char *l = a.maps + (size_t)(lo ? p.left_lo : p.left) * MUON_MAP_BYTES, *r = a.maps + (size_t)(lo ? p.right_lo : p.right) * MUON_MAP_BYTES;
                         tmap_acquire(l);
                         tmap_acquire(r);
-                        if (p.phase != MUON_GRAM) {
+                        if (TILE == 256 && p.phase != MUON_GRAM) {
                             tmap_acquire(l + MUON_MAP_MN * MUON_MAP_BYTES);
                             tmap_acquire(r + MUON_MAP_MN * MUON_MAP_BYTES);
                         }
@@ -736,7 +732,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                     break;
                 }
                 fence_proxy_async_all();  // what they wrote is read by this CTA's copies
-                if (CG == 2 && rank == 0) {
+                if (rank == 0) {
                     ok = wait_cluster(q_empty + 8 * slot, turn ^ 1);
                     if (!ok) break;
                     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(drawn_ring + slot), 1)), "r"(t) : "memory");
@@ -753,11 +749,11 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 arrive(r_full + 8 * slot);
                 next_slot();
                 if (t < 0) break;
-                const int row = tk.i * TILE + (int)rank * 128;
+                const int row = tk.i * TILE + (int)rank * ROWS;
                 // the epilogue will read the tile of the fp32 copies
                 for (int f = 0; f < (p.phase == MUON_GRAM ? 0 : p.phase == MUON_MUL ? 2 : 1); ++f)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < ROWS / 32; ++k) {
                         const int b = p.blocks - tk.j * (TILE / 32);
                         const unsigned bytes = (unsigned)(b < TILE / 32 ? b : TILE / 32) * 4096u;
                         const float *at = (f ? p.src2 : p.src) + ((size_t)(row / 32 + k) * p.blocks + tk.j * (TILE / 32)) * 1024;
@@ -773,122 +769,121 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             }
         }
     } else if (warp == 0) {
-        if (lane == 0) {
-            const uint32_t full0 = CG == 2 ? map_to_rank(full, 0) : full;
-            int stage = 0;
-            unsigned phase = 0, used = 0;
-            for (;;) {
-                ok = wait_local(r_full + 8 * slot, turn);
-                if (!ok) break;
-                const RingEntry &e = ring[slot];
-                const int end = e.end, kind = e.p.phase, steps = e.p.steps, parts = e.p.parts;
-                const char *left = a.maps + (size_t)e.p.left * MUON_MAP_BYTES, *right = a.maps + (size_t)e.p.right * MUON_MAP_BYTES;
-                const char *left_lo = a.maps + (size_t)e.p.left_lo * MUON_MAP_BYTES, *right_lo = a.maps + (size_t)e.p.right_lo * MUON_MAP_BYTES;
-                const int row = e.i * TILE + (int)rank * 128, col = e.j * TILE + (int)rank * 128;
-                const int left_rows = kind == MUON_GRAM ? 0 : e.i * TILE;  // from here on K's elements lie in the panel's rows
-                const int right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? e.j * TILE : 1 << 30;
-                arrive(r_empty + 8 * slot);
-                next_slot();
-                if (end) break;
-                int left_steps = steps * parts;
-                for (int k = 0; k < steps; ++k)
-                    for (int part = 0; ok && part < parts; ++part) {  // hi, lo
-                        const char *ml = part ? left_lo : left, *mr = part ? right_lo : right;
-                        if (left_steps-- == min(steps * parts, NEAR_STEPS)) arrive(near_end);
-                        ok = wait_local(empty + 8 * stage, phase ^ 1);
-                        if (!ok) break;
-                        const uint32_t bar = full0 + 8 * stage, A = base + stage * STAGE, B = A + OPERAND;
-                        if (rank == 0) mbar_expect_tx(full + 8 * stage, CG * STAGE);
-                        if (64 * k >= left_rows)
-                            load_rows<CG>(A, ml, 64 * k, row, bar);
-                        else
-                            load_columns<CG>(A, ml + MUON_MAP_MN * MUON_MAP_BYTES, row, 64 * k, bar);
-                        if (64 * k >= right_rows)
-                            load_rows<CG>(B, mr, 64 * k, col, bar);
-                        else
-                            load_columns<CG>(B, mr + MUON_MAP_MN * MUON_MAP_BYTES, col, 64 * k, bar);
-                        ++used;
-                        if (++stage == STAGES) stage = 0, phase ^= 1;
+        const uint32_t full0 = map_to_rank(full, 0);
+        const bool one = elect_one();
+        int stage = 0;
+        unsigned phase = 0, used = 0;
+        for (;;) {
+            ok = all_of(wait_local(r_full + 8 * slot, turn));
+            if (!ok) break;
+            const RingEntry &e = ring[slot];
+            const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = uniform(e.p.parts), ti = uniform(e.i), tj = uniform(e.j);
+            const char *left = a.maps + (size_t)uniform(e.p.left) * MUON_MAP_BYTES, *right = a.maps + (size_t)uniform(e.p.right) * MUON_MAP_BYTES;
+            const char *left_lo = a.maps + (size_t)uniform(e.p.left_lo) * MUON_MAP_BYTES, *right_lo = a.maps + (size_t)uniform(e.p.right_lo) * MUON_MAP_BYTES;
+            const int row = ti * TILE + (int)rank * ROWS, col = tj * TILE + (int)rank * ROWS;
+            const int left_rows = kind == MUON_GRAM ? 0 : ti * TILE;  // from here on K's elements lie in the panel's rows
+            const int right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? tj * TILE : 1 << 30;
+            __syncwarp();
+            if (one) arrive(r_empty + 8 * slot);
+            next_slot();
+            if (end) break;
+            int left_steps = steps * parts;
+            const int near_steps = min(left_steps, NEAR_STEPS);
+            for (int k = 0; ok && k < steps; ++k)
+                for (int part = 0; part < parts; ++part) {  // hi, lo
+                    const char *ml = part ? left_lo : left, *mr = part ? right_lo : right;
+                    if (left_steps-- == near_steps && one) arrive(near_end);
+                    ok = all_of(wait_local(empty + 8 * stage, phase ^ 1));
+                    if (!ok) break;
+                    const uint32_t bar = full0 + 8 * stage, A = base + stage * STAGE, B = A + OPERAND;
+                    if (one) {
+                        if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * STAGE);
+                        load_operand<ROWS>(A, ml, 64 * k < left_rows, row, 64 * k, bar);
+                        load_operand<ROWS>(B, mr, 64 * k < right_rows, col, 64 * k, bar);
                     }
-                if (!ok) break;
-            }
-            // before the CTA ends, every stage has been read (after a failure: waited for, as long as a wait lasts)
-            for (int s = 0; s < STAGES && used; ++s) {
-                if (used >= (unsigned)STAGES || s < stage) {
-                    const unsigned last = s < stage ? phase : phase ^ 1;
-                    if (!wait_local(empty + 8 * s, last)) ok = false;
+                    ++used;
+                    if (++stage == STAGES) stage = 0, phase ^= 1;
                 }
+            if (!ok) break;
+        }
+        // before the CTA ends, every stage has been read (after a failure: waited for, as long as a wait lasts)
+        for (int s = 0; s < STAGES && used; ++s) {
+            if (used >= (unsigned)STAGES || s < stage) {
+                const unsigned last = s < stage ? phase : phase ^ 1;
+                if (!wait_local(empty + 8 * s, last)) ok = false;
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
+            const bool one = elect_one();
             int stage = 0, n_done = 0;
             unsigned phase = 0;
             for (;; ++n_done) {
-                ok = wait_local(r_full + 8 * slot, turn);
+                ok = all_of(wait_local(r_full + 8 * slot, turn));
                 if (!ok) break;
                 const RingEntry &e = ring[slot];
-                const int end = e.end, kind = e.p.phase, steps = e.p.steps, parts = e.p.parts;
-                const int left_rows = kind == MUON_GRAM ? 0 : e.i * TILE, right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? e.j * TILE : 1 << 30;
-                arrive(r_empty + 8 * slot);
+                const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = uniform(e.p.parts), ti = uniform(e.i), tj = uniform(e.j);
+                const int left_rows = kind == MUON_GRAM ? 0 : ti * TILE, right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? tj * TILE : 1 << 30;
+                __syncwarp();
+                if (one) arrive(r_empty + 8 * slot);
                 next_slot();
                 if (end) break;
                 const int acc = n_done & 1;
-                ok = CG == 2 ? wait_cluster(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1) : wait_local(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1);
+                ok = all_of(wait_cluster(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1));
                 if (!ok) break;
                 tc_after();
                 const uint32_t d = tmem + acc * 256;
-                uint32_t accumulate = 0;
+                // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row.  MN-major: blocks of 64 columns
+                // 8192 bytes apart, groups of 8 rows of K 1024.
+                auto multiply = [&](uint64_t da, uint64_t db, uint32_t idesc, uint32_t a_step, uint32_t b_step, uint32_t accumulate) {
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) mma_f16(d, da + kk * a_step, db + kk * b_step, idesc, kk ? 1u : accumulate);
+                };
                 for (int k = 0; k < steps; ++k) {
-                    // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row.  MN-major: blocks of 64
-                    // columns 8192 bytes apart, groups of 8 rows of K 1024.
                     const bool a_mn = 64 * k < left_rows, b_mn = 64 * k < right_rows;
                     const uint32_t idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
-                    const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
-                    auto multiply = [&](int sa, int sb) {
-                        uint64_t da = operand_desc(base + sa * STAGE, a_mn ? 8192 : 16, 1024), db = operand_desc(base + sb * STAGE + OPERAND, b_mn ? 8192 : 16, 1024);
-#pragma unroll
-                        for (int kk = 0; kk < 4; ++kk) {
-                            mma_f16<CG>(d, da, db, idesc, accumulate);
-                            accumulate = 1;
-                            da += a_step;
-                            db += b_step;
-                        }
-                    };
-                    ok = wait_local(full + 8 * stage, phase);
+                    const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+                    const uint64_t a_at = operand_desc(0, a_mn ? 8192 : 16, 1024), b_at = operand_desc(0, b_mn ? 8192 : 16, 1024);
+                    const uint32_t at = (base + stage * STAGE) >> 4;  // (below 2^14)
+                    const uint64_t da = a_at + at, db = b_at + at + (OPERAND >> 4);
+                    ok = all_of(wait_local(full + 8 * stage, phase));
                     if (!ok) break;
                     tc_after();
                     const int hi = stage;
-                    multiply(hi, hi);
+                    if (one) multiply(da, db, idesc, a_step, b_step, k ? 1u : 0u);
                     if (++stage == STAGES) stage = 0, phase ^= 1;
                     if (parts > 1) {  // the next stage holds the lo parts
-                        ok = wait_local(full + 8 * stage, phase);
+                        ok = all_of(wait_local(full + 8 * stage, phase));
                         if (!ok) break;
                         tc_after();
-                        multiply(hi, stage);
-                        multiply(stage, hi);
-                        mma_commit<CG>(empty + 8 * hi);
-                        mma_commit<CG>(empty + 8 * stage);
+                        const uint32_t at_lo = (base + stage * STAGE) >> 4;
+                        if (one) {
+                            multiply(da, b_at + at_lo + (OPERAND >> 4), idesc, a_step, b_step, 1u);
+                            multiply(a_at + at_lo, db, idesc, a_step, b_step, 1u);
+                            mma_commit(empty + 8 * hi);
+                            mma_commit(empty + 8 * stage);
+                        }
                         if (++stage == STAGES) stage = 0, phase ^= 1;
-                    } else {
-                        mma_commit<CG>(empty + 8 * hi);
+                    } else if (one) {
+                        mma_commit(empty + 8 * hi);
                     }
                 }
                 if (!ok) break;
-                mma_commit<CG>(t_full + 8 * acc);
+                if (one) mma_commit(t_full + 8 * acc);
             }
             if (!ok) {  // what was issued ends before the tensor memory is freed
-                if constexpr (CG == 1)
-                    mma_commit<1>(drained);
-                else
+                if (one)
                     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(drained) : "memory");
                 mbar_wait_bounded(drained, 0);
             }
         }
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;  // a warp reads the lanes 32 (warp % 4) .. + 31; the two of a quarter share its columns
-        const uint32_t t_empty0 = CG == 2 ? map_to_rank(t_empty, 0) : t_empty;
-        float *st = reinterpret_cast<float *>(raw + (base - raw_s) + STAGES * STAGE) + (warp - 2) * 1024;
+        // a warp reads the lanes 32 (warp % 4) .. + 31; the two of a quarter share its columns
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        constexpr int BLOCKS = TILE == 256 ? 4 : 1;
+        const int warp_row = (int)rank * ROWS + 32 * (TILE == 256 ? q : q & 1), warp_column = half * (32 * BLOCKS) + (TILE == 256 ? 0 : 64 * (q >> 1));
+        const uint32_t t_empty0 = map_to_rank(t_empty, 0);
+        float *st = reinterpret_cast<float *>(raw + (base - raw_s) + RING_BYTES) + (warp - 2) * 1024;
         int out_turn = 0;
         unsigned *told = nullptr;  // the counter that is still to be told of this warp's last task
         // The copies are written; with them and this warp's other stores the completion is told.  It waits for memory, so that it comes when
@@ -912,8 +907,8 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             const int ti = ring[slot].i, tj = ring[slot].j;
             if (ring[slot].end) break;
             next_slot();
-            const int r0 = ti * TILE + (int)rank * 128 + q * 32, first = tj * TILE + half * (TILE / 2);
-            const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 31) / 32, TILE / 64) : 0;
+            const int r0 = ti * TILE + warp_row, first = tj * TILE + warp_column;
+            const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 31) / 32, BLOCKS) : 0;
             const int acc = n_done & 1;
             const size_t at = ((size_t)(r0 / 32) * t.blocks + first / 32) * 1024 + lane * 4;
             float4 x[8], next[8];
@@ -945,7 +940,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                         load_block(t.src + at + (b + 1) * 1024, next);
                         if (t.phase <= MUON_MUL) next_column = __ldcg(t.vec2 + first + 32 * (b + 1) + lane);
                     }
-                    use(BlockAt{t.src2 + at + b * 1024, t.dst + at + b * 1024, tmem + acc * 256 + half * (TILE / 2) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, column, st});
+                    use(BlockAt{t.src2 + at + b * 1024, t.dst + at + b * 1024, tmem + acc * 256 + half * (32 * BLOCKS) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, column, st});
                 }
             };
             if (t.phase == MUON_GRAM)
@@ -960,12 +955,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 each_block([&](const BlockAt &b) { block_final(a, t, b, x, row); });
             tc_before();
             __syncwarp();
-            if (lane == 0) {
-                if (CG == 2)
-                    arrive_cluster(t_empty0 + 8 * acc);
-                else
-                    arrive(t_empty0 + 8 * acc);
-            }
+            if (lane == 0) arrive_cluster(t_empty0 + 8 * acc);
             if (t.phase != MUON_FINAL) told = a.done + t.mat;
             __syncwarp();
             if (lane == 0) arrive(slot_empty);
@@ -976,38 +966,34 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
     __syncwarp();
     tc_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();
+    cluster_sync();
     if (warp == 0) {
         tc_after();
-        if constexpr (CG == 1)
-            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
-        else
-            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     }
 }
 
-template <int CG>
+template <int TILE>
 cudaError_t launch_products(const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
 {
-    const void *kernel = reinterpret_cast<const void *>(muon_products_kernel<CG>);
+    const void *kernel = reinterpret_cast<const void *>(muon_products_kernel<TILE>);
     cudaError_t err = demo_allow_smem(dev, kernel);
     if (err != cudaSuccess) return err;
-    const int grid = workers * CG;
     MuonArgs args = a;
     void *params[] = {&args, &products, &tasks, &n_tasks};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.x = 2;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = dim3((unsigned)workers * 2u);
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = SMEM;
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = CG == 2 ? 2 : 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelExC(&cfg, kernel, params);
 }
 
@@ -1027,7 +1013,7 @@ cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_til
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_pack_kernel), n_tiles, NORM_THREADS, 0, stream, params);
 }
 
-cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
+cudaError_t muon_launch_products(int tile, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
 {
-    return pair ? launch_products<2>(a, products, tasks, n_tasks, workers, dev, stream) : launch_products<1>(a, products, tasks, n_tasks, workers, dev, stream);
+    return tile == 256 ? launch_products<256>(a, products, tasks, n_tasks, workers, dev, stream) : launch_products<128>(a, products, tasks, n_tasks, workers, dev, stream);
 }

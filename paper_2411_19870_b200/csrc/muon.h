@@ -112,6 +112,6 @@ struct MuonArgs {
 cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n_pieces, DemoLaunch &dev, cudaStream_t stream);
 // X = S u / (||u|| + eps), as hi + lo; clears the counters of the matrices [first_mat, first_mat + n_mats) and the next task.
 cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, DemoLaunch &dev, cudaStream_t stream);
-// All products.  pair: tiles of 256 x 256 by clusters of two CTAs; otherwise 128 x 128 by one.
-cudaError_t muon_launch_products(bool pair, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
+// All products, in tiles of 256 x 256 or 128 x 128, by pairs of CTAs.
+cudaError_t muon_launch_products(int tile, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
 constexpr int MUON_EPI_WARPS = 8;  // completions of a task: one for each of them in every CTA

@@ -19,7 +19,7 @@ namespace {
 // Matrices that are in the workspace together: a launch for their norms, one to lay them out and one for all their products.
 struct Group {
     int first_mat, n_mats, n_pieces;
-    bool pair;             // tiles of 256 x 256
+    int tile;              // side of the tiles
     long long pack_tiles;  // first of its list
     int n_pack;
     long long tasks;
@@ -140,7 +140,7 @@ void rebase(MuonMat &m, char *base)
     }
 }
 
-bool uses_pairs(const MuonMat &m) { return m.m > PRECISE_SIDE; }
+int tile_of(const MuonMat &m) { return m.m > PRECISE_SIDE ? 256 : 128; }
 
 // Two iterations in one (kernels_muon.cu) take 3 r + 5 products of m^3 multiplications, one after the other 6 r + 2, r = n / m.
 bool in_twos(const MuonMat &m, int steps) { return !m.precise && steps >= 3 && 2LL * m.n >= 3LL * m.m; }
@@ -234,9 +234,9 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
 // every product matrix by matrix: with two rounds of the workers' tasks in a cohort's symmetric products, a matrix's next product starts when its last
 // is done, and the X of a cohort of small matrices stays in L2.  Returns how many workers the tasks keep busy: more would take turns, and every one of
 // them would come with cold instruction caches (one 256 x 512: 70 workers 155 us, 8 XXX).
-int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, bool pair, Plan *plan)
+int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int side, Plan *plan)
 {
-    const int side = pair ? 256 : 128, ctas = pair ? 2 : 1, workers = std::max(1, c->launch.sm_count / ctas);
+    const int workers = std::max(1, c->launch.sm_count / 2);
     auto symmetric = [&](const MuonMat &m) { const long long k = ceil_div(m.m, side); return k * (k + 1) / 2; };
     long long total = 0;
     for (int e = 0; e < n; ++e) total += symmetric(mats[e]);
@@ -263,7 +263,7 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, boo
                 const size_t begin = plan->tasks.size();
                 each_tile(ceil_div(t.m, side), ceil_div(t.width, side), t.phase < MUON_UPDATE,
                           [&](int i, int j) { plan->tasks.push_back(MuonTask{product, (short)i, (short)j}); });
-                completed[e] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(ctas * MUON_EPI_WARPS);
+                completed[e] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(2 * MUON_EPI_WARPS);
             }
             most = std::max(most, plan->tasks.size() - step);
         }
@@ -294,15 +294,15 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
                                                            : 1.0f;
     }
     // groups hold matrices of one kind of tile
-    std::stable_sort(all.begin(), all.end(), [](const MuonMat &x, const MuonMat &y) { return uses_pairs(x) > uses_pairs(y); });
+    std::stable_sort(all.begin(), all.end(), [](const MuonMat &x, const MuonMat &y) { return tile_of(x) > tile_of(y); });
     for (size_t at = 0; at < all.size();) {
         Group g;
         std::memset(&g, 0, sizeof(g));
         g.first_mat = (int)at;
-        g.pair = uses_pairs(all[at]);
+        g.tile = tile_of(all[at]);
         long long elements = 0, pieces = 0;
         size_t work = 0, end = at;
-        for (; end < all.size() && uses_pairs(all[end]) == g.pair; ++end) {
+        for (; end < all.size() && tile_of(all[end]) == g.tile; ++end) {
             MuonMat &m = all[end];
             const long long n = (long long)m.m * m.n;
             if (end > at && elements + n > GROUP_ELEMENTS) break;
@@ -335,7 +335,7 @@ demo_status make_tasks(demo_muon_ctx *c, Plan *plan)
 {
     for (Group &g : c->groups) {
         g.tasks = (long long)plan->tasks.size();
-        g.workers = add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.pair, plan);
+        g.workers = add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.tile, plan);
         g.n_tasks = (int)((long long)plan->tasks.size() - g.tasks);
         if (plan->tasks.size() > (size_t)(1LL << 30)) return DEMO_ERR_UNSUPPORTED;
     }
@@ -343,7 +343,7 @@ demo_status make_tasks(demo_muon_ctx *c, Plan *plan)
 }
 
 // The three maps of a matrix of fp16 elements: see MUON_MAPS.
-bool encode_maps(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, void *base, long long cols, long long rows, long long ld)
+bool encode_maps(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, int tile, void *base, long long cols, long long rows, long long ld)
 {
     auto make = [&](CUtensorMap *to, int dims, const cuuint64_t *extent, const cuuint64_t *stride, const cuuint32_t *box, CUtensorMapSwizzle swizzle) {
         const cuuint32_t ones[3] = {1, 1, 1};
@@ -351,7 +351,7 @@ bool encode_maps(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, void *base
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     const cuuint64_t flat[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, row[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t panel[2] = {64, 128}, block[2] = {32, 32};
+    const cuuint32_t panel[2] = {64, (cuuint32_t)tile / 2}, block[2] = {32, 32};
     // blocks of 64 columns as the last axis (pad columns are read: they only reach results outside the matrix)
     const cuuint64_t cut[3] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64)}, cut_stride[2] = {(cuuint64_t)ld * 2, 128};
     const cuuint32_t two[3] = {64, 64, 2};
@@ -402,9 +402,9 @@ demo_status build(demo_muon_ctx *c)
     for (MuonMat &m : plan.mats) {
         CUtensorMap *p = &maps[(size_t)m.maps];
         for (int k = 0; k < 2; ++k)
-            ok = ok && encode_maps(encode, p + MUON_MAP_X + k, m.xhi[k], m.n, m.m, m.ldx) && encode_maps(encode, p + MUON_MAP_XLO + k, m.xlo[k], m.n, m.m, m.ldx);
+            ok = ok && encode_maps(encode, p + MUON_MAP_X + k, tile_of(m), m.xhi[k], m.n, m.m, m.ldx) && encode_maps(encode, p + MUON_MAP_XLO + k, tile_of(m), m.xlo[k], m.n, m.m, m.ldx);
         for (int k = 0; k < m.symmetric; ++k)
-            ok = ok && encode_maps(encode, p + MUON_MAP_E + k, m.ehi[k], m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_ELO + k, m.elo[k], m.m, m.m, m.lde);
+            ok = ok && encode_maps(encode, p + MUON_MAP_E + k, tile_of(m), m.ehi[k], m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_ELO + k, tile_of(m), m.elo[k], m.m, m.m, m.lde);
     }
     if (!ok) return DEMO_ERR_CUDA;
     ok = cudaMemcpy(c->d_mats, plan.mats.data(), T * sizeof(MuonMat), cudaMemcpyHostToDevice) == cudaSuccess &&
@@ -466,7 +466,7 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     for (const Group &grp : c->groups) {
         if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, stream);
         if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, c->launch, stream);
-        if (err == cudaSuccess) err = muon_launch_products(grp.pair, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, stream);
+        if (err == cudaSuccess) err = muon_launch_products(grp.tile, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, stream);
         c->launches += 3;
     }
     if (err != cudaSuccess) {
