@@ -248,8 +248,8 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
 // ---- products -----------------------------------------------------------------------------------------------------------------
 
 constexpr int EPI_WARPS = MUON_EPI_WARPS;
-constexpr int SCHEDULER = EPI_WARPS + 2;       // its warp
-constexpr int THREADS = 96 + 32 * EPI_WARPS;  // loading warp, MMA warp, epilogue, scheduler
+constexpr int SCHEDULER = EPI_WARPS + 2, LOAD_RIGHT = EPI_WARPS + 3;  // their warps
+constexpr int THREADS = 128 + 32 * EPI_WARPS;  // loads of the left operand, MMAs, epilogue, scheduler, loads of the right operand
 constexpr int RING_BYTES = 6 * 32768;         // of operands: steps of K = 64, both operands of a CTA
 constexpr int TMEM_COLS = 512;
 constexpr int SMEM = RING_BYTES + EPI_WARPS * 4096 + 1024;
@@ -630,7 +630,7 @@ struct alignas(16) RingEntry {
 
 // All products of all iterations, by persistent workers, pairs of CTAs.  Tasks are drawn in the list's order from one counter, so
 // whatever a task waits for is done already or in the hands of a worker that runs: no worker has to be resident for another to go on.
-// One warp loads, one issues the MMAs, eight read accumulators back: two of them, so that the products of a task run beside the epilogue
+// Two warps load, one each operand, one issues the MMAs, eight read accumulators back: two of them, so that the products of a task run beside the epilogue
 // of the one before.  A fourth kind of warp schedules: that of a worker's first CTA draws the tasks and waits until they may start, and in
 // both CTAs it puts what the others need to know of one into a ring, up to four ahead (by the loading warp itself: its look-ups and waits,
 // 3500 cycles a task, leave the tensor core without data).
@@ -655,7 +655,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                    r_empty = r_full + 8 * RING, q_full = r_empty + 8 * RING, q_empty = q_full + 8 * RING, near_end = q_empty + 8 * RING, drained = near_end + 8;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
-            mbar_init(full + 8 * s, 1);
+            mbar_init(full + 8 * s, 2);  // a loading warp each of the first CTA
             mbar_init(empty + 8 * s, 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
         }
         for (int s = 0; s < RING; ++s) {
             mbar_init(r_full + 8 * s, 1);
-            mbar_init(r_empty + 8 * s, EPI_WARPS + (rank == 0 ? 2 : 1));  // the epilogues, the loading warp and the first CTA's MMA warp
+            mbar_init(r_empty + 8 * s, EPI_WARPS + (rank == 0 ? 3 : 2));  // the epilogues, the loading warps and the first CTA's MMA warp
             mbar_init(q_full + 8 * s, 1);
             mbar_init(q_empty + 8 * s, 1);
         }
@@ -768,7 +768,8 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 }
             }
         }
-    } else if (warp == 0) {
+    } else if (warp == 0 || warp == LOAD_RIGHT) {
+        const bool left_side = warp == 0;
         const uint32_t full0 = map_to_rank(full, 0);
         const bool one = elect_one();
         int stage = 0;
@@ -778,11 +779,11 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             if (!ok) break;
             const RingEntry &e = ring[slot];
             const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = uniform(e.p.parts), ti = uniform(e.i), tj = uniform(e.j);
-            const char *left = a.maps + (size_t)uniform(e.p.left) * MUON_MAP_BYTES, *right = a.maps + (size_t)uniform(e.p.right) * MUON_MAP_BYTES;
-            const char *left_lo = a.maps + (size_t)uniform(e.p.left_lo) * MUON_MAP_BYTES, *right_lo = a.maps + (size_t)uniform(e.p.right_lo) * MUON_MAP_BYTES;
-            const int row = ti * TILE + (int)rank * ROWS, col = tj * TILE + (int)rank * ROWS;
-            const int left_rows = kind == MUON_GRAM ? 0 : ti * TILE;  // from here on K's elements lie in the panel's rows
-            const int right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? tj * TILE : 1 << 30;
+            const char *hi = a.maps + (size_t)uniform(left_side ? e.p.left : e.p.right) * MUON_MAP_BYTES;
+            const char *lo = a.maps + (size_t)uniform(left_side ? e.p.left_lo : e.p.right_lo) * MUON_MAP_BYTES;
+            const int panel = (left_side ? ti : tj) * TILE, at = panel + (int)rank * ROWS;
+            // from here on K's elements lie in the panel's rows
+            const int rows_from = kind == MUON_GRAM ? 0 : left_side || kind <= MUON_MUL ? panel : 1 << 30;
             __syncwarp();
             if (one) arrive(r_empty + 8 * slot);
             next_slot();
@@ -791,15 +792,12 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             const int near_steps = min(left_steps, NEAR_STEPS);
             for (int k = 0; ok && k < steps; ++k)
                 for (int part = 0; part < parts; ++part) {  // hi, lo
-                    const char *ml = part ? left_lo : left, *mr = part ? right_lo : right;
-                    if (left_steps-- == near_steps && one) arrive(near_end);
+                    if (left_steps-- == near_steps && one && left_side) arrive(near_end);
                     ok = all_of(wait_local(empty + 8 * stage, phase ^ 1));
                     if (!ok) break;
-                    const uint32_t bar = full0 + 8 * stage, A = base + stage * STAGE, B = A + OPERAND;
                     if (one) {
-                        if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * STAGE);
-                        load_operand<ROWS>(A, ml, 64 * k < left_rows, row, 64 * k, bar);
-                        load_operand<ROWS>(B, mr, 64 * k < right_rows, col, 64 * k, bar);
+                        if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * OPERAND);
+                        load_operand<ROWS>(base + stage * STAGE + (left_side ? 0 : OPERAND), part ? lo : hi, 64 * k < rows_from, at, 64 * k, full0 + 8 * stage);
                     }
                     ++used;
                     if (++stage == STAGES) stage = 0, phase ^= 1;
