@@ -621,7 +621,7 @@ __device__ __forceinline__ bool wait_task(const unsigned *done, unsigned need, c
     }
     return true;
 }
-__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
 struct alignas(16) RingEntry {
     MuonProduct p;
@@ -644,7 +644,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
     constexpr int ROWS = TILE / 2, OPERAND = ROWS * 128, STAGE = 2 * OPERAND, STAGES = RING_BYTES / STAGE;
     constexpr int RING = 4, NEAR_STEPS = 8;
     extern __shared__ unsigned char raw[];
-    __shared__ unsigned long long bars[2 * STAGES + 4 + 4 * RING + 2];
+    __shared__ unsigned long long bars[2 * STAGES + 4 + 5 * RING + 2];
     __shared__ RingEntry ring[RING];
     __shared__ int drawn_ring[RING];
     __shared__ uint32_t tmem_slot;
@@ -652,7 +652,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, t_full = empty + 8 * STAGES, t_empty = t_full + 16, r_full = t_empty + 16,
-                   r_empty = r_full + 8 * RING, q_full = r_empty + 8 * RING, q_empty = q_full + 8 * RING, near_end = q_empty + 8 * RING, drained = near_end + 8;
+                   r_empty = r_full + 8 * RING, q_full = r_empty + 8 * RING, q_empty = q_full + 8 * RING, go_full = q_empty + 8 * RING, near_end = go_full + 8 * RING, drained = near_end + 8;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(full + 8 * s, 2);  // a loading warp each of the first CTA
@@ -667,6 +667,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             mbar_init(r_empty + 8 * s, EPI_WARPS + (rank == 0 ? 3 : 2));  // the epilogues, the loading warps and the first CTA's MMA warp
             mbar_init(q_full + 8 * s, 1);
             mbar_init(q_empty + 8 * s, 1);
+            mbar_init(go_full + 8 * s, 1);
         }
         mbar_init(near_end, 1);
         mbar_init(drained, 1);
@@ -699,6 +700,11 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 int t;
                 if (rank == 0) {
                     t = drawn < (unsigned)n_tasks ? (int)drawn : -1;
+                    // the second CTA looks the task up, too, while this one waits for what the task needs
+                    ok = wait_cluster(q_empty + 8 * slot, turn ^ 1);
+                    if (!ok) break;
+                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(drawn_ring + slot), 1)), "r"(t) : "memory");
+                    arrive_release_cluster(map_to_rank(q_full + 8 * slot, 1));
                 } else {
                     ok = wait_cluster(q_full + 8 * slot, turn);
                     if (!ok) break;
@@ -727,17 +733,15 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                         if (p.phase != MUON_FINAL) tmap_acquire(a.maps + (size_t)(lo ? p.out_lo : p.out) * MUON_MAP_BYTES);
                     }
                 }
-                if (rank == 0 && t >= 0 && !wait_task(a.done + p.mat, p.need, a.status)) {
-                    ok = false;
-                    break;
-                }
-                fence_proxy_async_all();  // what they wrote is read by this CTA's copies
                 if (rank == 0) {
-                    ok = wait_cluster(q_empty + 8 * slot, turn ^ 1);
+                    ok = t < 0 || wait_task(a.done + p.mat, p.need, a.status);
                     if (!ok) break;
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(drawn_ring + slot), 1)), "r"(t) : "memory");
-                    arrive_release_cluster(map_to_rank(q_full + 8 * slot, 1));
+                    arrive_release_cluster(map_to_rank(go_full + 8 * slot, 1));
+                } else {
+                    ok = wait_cluster(go_full + 8 * slot, turn);
+                    if (!ok) break;
                 }
+                fence_proxy_async_global();  // what other tasks wrote is read by this CTA's copies
                 ok = wait_local(r_empty + 8 * slot, turn ^ 1);
                 if (!ok) break;
                 {
@@ -889,7 +893,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
         auto tell = [&] {
             if (lane == 0 && told) {
                 asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-                fence_proxy_async_all();
+                fence_proxy_async_global();
                 asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(told), "r"(1u) : "memory");
             }
             told = nullptr;
