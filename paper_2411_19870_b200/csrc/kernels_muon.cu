@@ -247,12 +247,15 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
 
 // ---- products -----------------------------------------------------------------------------------------------------------------
 
-constexpr int EPI_WARPS = MUON_EPI_WARPS;
-constexpr int SCHEDULER = EPI_WARPS + 2, LOAD_RIGHT = EPI_WARPS + 3;  // their warps
-constexpr int THREADS = 128 + 32 * EPI_WARPS;  // loads of the left operand, MMAs, epilogue, scheduler, loads of the right operand
-constexpr int RING_BYTES = 6 * 32768;         // of operands: steps of K = 64, both operands of a CTA
+constexpr int MMA = 1, SCHEDULER = 2, LOAD_RIGHT = 3, FIRST_EPI = 4;  // warps; warp 0 loads the left operand
 constexpr int TMEM_COLS = 512;
-constexpr int SMEM = RING_BYTES + EPI_WARPS * 4096 + 1024;
+template <int TILE>
+struct Shape {
+    static constexpr int EPI_WARPS = muon_epilogue_warps(TILE), THREADS = 32 * (FIRST_EPI + EPI_WARPS);
+    // a CTA's rows of both operands of a step of K = 64, as many steps as there is room for beside 4 KB for each warp of the epilogue
+    static constexpr int ROWS = TILE / 2, OPERAND = ROWS * 128, STAGE = 2 * OPERAND, STAGES = (224 * 1024 - EPI_WARPS * 4096) / STAGE;
+    static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * 4096 + 1024;
+};
 
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -359,15 +362,24 @@ __device__ __forceinline__ bool wait_cluster(uint32_t bar, unsigned parity)
     }
 }
 
-// A warp's block of 32 x 32 accumulators on its way through shared memory, from a row a lane, as tensor memory gives it, to pieces of eight
-// columns, as memory wants it: four lanes then cover 32 columns of a row.  16-byte quads are stored where neither the rows' writes, nor the
-// pieces' reads, nor reads down the columns meet in a bank.
-__device__ __forceinline__ int quad_at(int row, int quad) { return row * 32 + ((quad ^ (row & 7) ^ ((row >> 3) << 1)) << 2); }
-__device__ __forceinline__ void stage_rows(float *st, const float (&v)[32], int lane)
+// ---- epilogues: a warp's block is 32 rows, a lane's row, by 16 columns ---------------------------------------------------------
+
+// 16 consecutive fp32 columns of this thread's tensor-memory lane.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16])
 {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) *reinterpret_cast<float4 *>(st + quad_at(lane, k)) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+          "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(taddr)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
+
+// 32 x 32 results on their way to the caller's tensor pass through shared memory, from a row a lane to pieces of eight columns: four lanes then
+// cover 32 columns of a row.  16-byte quads are stored where neither the rows' writes, nor the pieces' reads, nor reads down the columns meet
+// in a bank.
+__device__ __forceinline__ int quad_at(int row, int quad) { return row * 32 + ((quad ^ (row & 7) ^ ((row >> 3) << 1)) << 2); }
 __device__ __forceinline__ void read_piece(const float *st, int row, int q, float (&v)[8])
 {
     const float4 a = *reinterpret_cast<const float4 *>(st + quad_at(row, 2 * q)), b = *reinterpret_cast<const float4 *>(st + quad_at(row, 2 * q + 1));
@@ -429,160 +441,160 @@ __device__ __forceinline__ void deliver(const MuonArgs &a, void *out, size_t at,
     }
 }
 
-// ---- epilogues: a warp's block is 32 rows, a lane's row, by 32 columns -------------------------------------------------------------
-
-// The fp16 values of a block on their way out: rows of 64 bytes, the 16-byte pieces of row r at piece ^ (r / 2 % 4), the 64-byte swizzle.
-__device__ __forceinline__ void stage_halves(unsigned char *buf, const uint32_t (&p)[16], int lane)
+// (past the L1, which may hold these addresses as they were an iteration ago)
+__device__ __forceinline__ void load_block(const float *p, float4 (&x)[4])
 {
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<uint4 *>(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
+    for (int k = 0; k < 4; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(p + k * 128));
 }
+__device__ __forceinline__ void store_block(float *p, const float (&v)[16])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) __stcg(reinterpret_cast<float4 *>(p + k * 128), make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
+}
+__device__ __forceinline__ float part(const float4 (&x)[4], int k) { return reinterpret_cast<const float *>(x)[k]; }
+
 struct BlockAt {
-    const float *src2;  // the lane's place in the block of the right factor's fp32 copy
-    float *dst;         // and of the result's
+    size_t fp32;   // the lane's place in the block of the fp32 copies
     uint32_t tmem;
-    int r0, j0, lane;
-    float column;       // POLY, MUL: the right factor's diagonal at column j0 + lane
-    float *st;          // the warp's 4 KB of shared memory
+    int r0, j0, number, lane;  // row and column of the result; the how-manieth of the warp's blocks
+    float column;  // POLY, MUL: the right factor's diagonal at column j0 + lane, lane < 16
+    unsigned char *st;  // the warp's 4 KB of shared memory
 };
 
-// Writes a block as fp16 and, where the products need it, what that leaves.  The copies read the buffers after this returns; two alternate.
-// (pad columns and rows: the copy leaves out what lies outside the matrix)
-__device__ __forceinline__ void write_halves(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float (&v)[32])
+// The fp16 values of a block into the warp's part of shared memory, from where one copy writes all of them: rows of 128 bytes, the 16-byte
+// pieces of row r at piece ^ (r % 8), or, in tiles of 128, where there are two blocks and the lo parts behind the hi parts, rows of 64 bytes at
+// piece ^ (r / 2 % 4).
+template <bool PRECISE>
+__device__ __forceinline__ void stage_halves(const BlockAt &b, const float (&v)[16])
 {
-    const bool precise = t.parts > 1;
-    const int lane = b.lane;
-    unsigned char *bufs = reinterpret_cast<unsigned char *>(b.st);
-    uint32_t p[16];
+    uint32_t p[8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) p[k] = pack2(v[2 * k], v[2 * k + 1]);
-    if (lane == 0) {
-        if (precise)
-            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-        else
-            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-    }
-    __syncwarp();
-    unsigned char *buf = bufs + (precise ? 0 : turn * 2048);
-    turn ^= 1;
-    stage_halves(buf, p, lane);
-    if (precise) {
+    for (int k = 0; k < 8; ++k) p[k] = pack2(v[2 * k], v[2 * k + 1]);
+    auto put = [&](unsigned char *at) {
+        const int swap = PRECISE ? b.lane >> 1 & 3 : b.lane & 7, piece = 2 * b.number;
+        unsigned char *row = at + b.lane * (PRECISE ? 64 : 128);
+        *reinterpret_cast<uint4 *>(row + ((piece ^ swap) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
+        *reinterpret_cast<uint4 *>(row + (((piece + 1) ^ swap) << 4)) = make_uint4(p[4], p[5], p[6], p[7]);
+    };
+    put(b.st);
+    if (PRECISE) {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
+        for (int k = 0; k < 8; ++k) {
             const float2 h = unpack2(p[k]);
             p[k] = pack2(v[2 * k] - h.x, v[2 * k + 1] - h.y);
         }
-        stage_halves(bufs + 2048, p, lane);
-    }
-    fence_proxy_async();
-    __syncwarp();
-    if (lane == 0) {
-        tma_store_2d(a.maps + (size_t)t.out * MUON_MAP_BYTES, b.j0, b.r0, smem_u32(buf));
-        if (precise) tma_store_2d(a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, b.j0, b.r0, smem_u32(bufs + 2048));
-        tma_store_commit();
+        put(b.st + 2048);
     }
 }
 
-// (past the L1, which may hold these addresses as they were an iteration ago)
-__device__ __forceinline__ void load_block(const float *p, float4 (&x)[8])
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(p + k * 128));
-}
-__device__ __forceinline__ void store_block(float *p, const float (&v)[32])
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) __stcg(reinterpret_cast<float4 *>(p + k * 128), make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
-}
-__device__ __forceinline__ const float &part(const float4 (&x)[8], int k) { return reinterpret_cast<const float *>(x)[k]; }
-
-// Is this block on the diagonal, its lane's own element is v[lane]: `own` takes it, and zero comes in its place.
-__device__ __forceinline__ float take_own(float (&v)[32], int lane)
+// The lane whose row meets the diagonal in this block takes its element out of it.
+__device__ __forceinline__ float take_own(const BlockAt &b, float (&v)[16])
 {
     float own = 0.f;
 #pragma unroll
-    for (int k = 0; k < 32; ++k)
-        if (k == lane) {
+    for (int k = 0; k < 16; ++k)
+        if (b.j0 + k == b.r0 + b.lane) {
             own = v[k];
             v[k] = 0.f;
         }
     return own;
 }
+__device__ __forceinline__ bool on_diagonal(const BlockAt &b) { return (b.r0 ^ b.j0) < 32; }  // (both below 2^31, multiples of 32 and 16)
+__device__ __forceinline__ bool has_own(const BlockAt &b) { return (unsigned)(b.r0 + b.lane - b.j0) < 16u; }
 
-__device__ __forceinline__ void block_gram(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn)
+// E = A off the diagonal, d on it.
+template <bool PRECISE>
+__device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &b)
 {
-    float v[32];
-    tmem_ld32(b.tmem, v);
+    float v[16];
+    tmem_ld16(b.tmem, v);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] *= t.scale;
-    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, take_own(v, b.lane) * MUON_EF_INV);
-    write_halves(a, t, b, turn, v);
-    store_block(b.dst, v);
+    for (int k = 0; k < 16; ++k) v[k] *= t.scale;
+    if (on_diagonal(b)) {
+        const float own = take_own(b, v);
+        if (has_own(b)) __stcg(t.diag + b.r0 + b.lane, own * MUON_EF_INV);
+    }
+    stage_halves<PRECISE>(b, v);
+    store_block(t.dst + b.fp32, v);
 }
 
 // B = a + b A + c A^2
-__device__ __forceinline__ void block_poly(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&e)[8], float di)
+template <bool PRECISE>
+__device__ __forceinline__ void block_poly(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, const float4 (&e)[4], float di)
 {
-    float v[32];
-    tmem_ld32(b.tmem, v);
-    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, a.a + fmaf(a.b, di, a.c * fmaf(di, di, take_own(v, b.lane) * (MUON_EF_INV * MUON_EF_INV))));
+    float v[16];
+    tmem_ld16(b.tmem, v);
+    if (on_diagonal(b)) {
+        const float own = take_own(b, v) * (MUON_EF_INV * MUON_EF_INV);
+        if (has_own(b)) __stcg(t.diag + b.r0 + b.lane, a.a + fmaf(a.b, di, a.c * fmaf(di, di, own)));
+    }
     const float base = fmaf(a.c, di, a.b), scale = a.c * MUON_EF_INV;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(fmaf(a.c, __shfl_sync(0xffffffffu, b.column, k), base), part(e, k), scale * v[k]);  // (E's own diagonal is zero)
-    write_halves(a, t, b, turn, v);
-    if (t.dst) store_block(b.dst, v);
+    for (int k = 0; k < 16; ++k) v[k] = fmaf(fmaf(a.c, __shfl_sync(0xffffffffu, b.column, k), base), part(e, k), scale * v[k]);  // (E's own diagonal is zero)
+    stage_halves<PRECISE>(b, v);
+    if (t.dst) store_block(t.dst + b.fp32, v);
 }
 
 // P Q, of matrices that commute
-__device__ __forceinline__ void block_mul(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&e)[8], float di)
+template <bool PRECISE>
+__device__ __forceinline__ void block_mul(const MuonProduct &t, const BlockAt &b, const float4 (&e)[4], float di)
 {
-    float v[32];
-    float4 f[8];
-    load_block(b.src2, f);
-    tmem_ld32(b.tmem, v);
-    if (b.r0 == b.j0) __stcg(t.diag + b.r0 + b.lane, fmaf(di, b.column, take_own(v, b.lane) * (MUON_EF_INV * MUON_EF_INV)));
+    float v[16];
+    float4 f[4];
+    load_block(t.src2 + b.fp32, f);
+    tmem_ld16(b.tmem, v);
+    const float dj = __shfl_sync(0xffffffffu, b.column, b.lane & 15);  // (of the lane's own element, where the block holds it)
+    if (on_diagonal(b)) {
+        const float own = take_own(b, v) * (MUON_EF_INV * MUON_EF_INV);
+        if (has_own(b)) __stcg(t.diag + b.r0 + b.lane, fmaf(di, dj, own));
+    }
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(f, k), v[k] * MUON_EF_INV);
-#pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(part(e, k), __shfl_sync(0xffffffffu, b.column, k), v[k]);
-    write_halves(a, t, b, turn, v);
-    if (t.dst) store_block(b.dst, v);
+    for (int k = 0; k < 16; ++k) v[k] = fmaf(di, part(f, k), fmaf(part(e, k), __shfl_sync(0xffffffffu, b.column, k), v[k] * MUON_EF_INV));
+    stage_halves<PRECISE>(b, v);
+    if (t.dst) store_block(t.dst + b.fp32, v);
 }
 
 // X <- B X
-__device__ __forceinline__ void block_update(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, int &turn, const float4 (&x)[8], float di)
+template <bool PRECISE>
+__device__ __forceinline__ void block_update(const MuonProduct &t, const BlockAt &b, const float4 (&x)[4], float di)
 {
-    float v[32];
-    tmem_ld32(b.tmem, v);
+    float v[16];
+    tmem_ld16(b.tmem, v);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV);
-    write_halves(a, t, b, turn, v);
-    store_block(b.dst, v);
+    for (int k = 0; k < 16; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV);
+    stage_halves<PRECISE>(b, v);
+    store_block(t.dst + b.fp32, v);
 }
 
-// The same, the last time: to the caller's tensor.
-__device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, const float4 (&x)[8], float di)
+// The same, the last time: to the caller's tensor, 32 columns at a time where the warp has them.  more: another 16 columns follow.
+__device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, const float4 (&x)[4], float di, bool more)
 {
     const bool params = a.to == MUON_TO_PARAMS;
     const float scale = params ? -a.lr * t.step_scale : t.scale, keep = 1.f - a.lr * a.wd;
     void *out = a.out[t.tensor];
-    // the lane's four pieces of the tensor: rows 8 i + lane / 4, eight columns; of X, where it is the transpose, the other way round
-    const int r0 = t.transposed ? b.j0 : b.r0, c = (t.transposed ? b.r0 : b.j0) + 8 * (b.lane & 3);
-    const int rows = t.transposed ? t.width : t.m, cols = t.transposed ? t.m : t.width;
-    const bool whole = whole_piece(a, c, cols);
+    float *st = reinterpret_cast<float *>(b.st);
+    const int half = b.number & 1;
     {
-        float v[32];
-        tmem_ld32(b.tmem, v);
+        float v[16];
+        tmem_ld16(b.tmem, v);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV) * scale;
-        stage_rows(b.st, v, b.lane);
+        for (int k = 0; k < 16; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV) * scale;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) *reinterpret_cast<float4 *>(st + quad_at(b.lane, 4 * half + k)) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
     }
+    if (!half && more) return;
+    __syncwarp();
+    // the lane's pieces of the tensor: rows 8 i + lane / 4, eight columns; of X, where it is the transpose, the other way round
+    const int j0 = b.j0 - 16 * half, wide = 16 * (half + 1), sub = b.lane >> 2, q = b.lane & 3;
+    const int r0 = t.transposed ? j0 : b.r0, c = (t.transposed ? b.r0 : j0) + 8 * q;
+    const int rows = min(t.transposed ? t.width : t.m, r0 + (t.transposed ? wide : 32)), cols = t.transposed ? t.m : t.width;
+    const bool mine = c < cols && (t.transposed || 8 * q < wide), whole = whole_piece(a, c, cols);
     float4 old[4][2];
-    if (params && whole) {
+    if (params && whole && mine) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = r0 + 8 * i + (b.lane >> 2);
+            const int r = r0 + 8 * i + sub;
             if (r < rows) {
                 const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(out) + (size_t)r * cols + c);
                 old[i][0] = from[0];
@@ -590,16 +602,16 @@ __device__ __forceinline__ void block_final(const MuonArgs &a, const MuonProduct
             }
         }
     }
-    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int r = r0 + 8 * i + (b.lane >> 2);
+        const int r = r0 + 8 * i + sub;
+        if (!mine || r >= rows) continue;
         float v[8];
         if (t.transposed)
-            read_column(b.st, 8 * i + (b.lane >> 2), b.lane & 3, v);
+            read_column(st, 8 * i + sub, q, v);
         else
-            read_piece(b.st, 8 * i + (b.lane >> 2), b.lane & 3, v);
-        if (r < rows && c < cols) deliver(a, out, (size_t)r * cols + c, cols - c, whole, v, keep, old[i]);
+            read_piece(st, 8 * i + sub, q, v);
+        deliver(a, out, (size_t)r * cols + c, cols - c, whole, v, keep, old[i]);
     }
     __syncwarp();
 }
@@ -638,10 +650,10 @@ struct alignas(16) RingEntry {
 // A worker's tile is TILE x TILE: 256, of which each CTA's tensor memory holds half the rows, or 128, for small matrices: of its 64 rows a CTA
 // then holds the left 64 columns in lanes 0 .. 63 and the right ones in lanes 64 .. 127.
 template <int TILE>
-__global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
+__global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
 {
     const StreamOrder order(1);
-    constexpr int ROWS = TILE / 2, OPERAND = ROWS * 128, STAGE = 2 * OPERAND, STAGES = RING_BYTES / STAGE;
+    constexpr int ROWS = Shape<TILE>::ROWS, OPERAND = Shape<TILE>::OPERAND, STAGE = Shape<TILE>::STAGE, STAGES = Shape<TILE>::STAGES, EPI_WARPS = Shape<TILE>::EPI_WARPS;
     constexpr int RING = 4, NEAR_STEPS = 8;
     extern __shared__ unsigned char raw[];
     __shared__ unsigned long long bars[2 * STAGES + 4 + 5 * RING + 2];
@@ -815,7 +827,7 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
                 if (!wait_local(empty + 8 * s, last)) ok = false;
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == MMA) {
         if (rank == 0) {
             const bool one = elect_one();
             int stage = 0, n_done = 0;
@@ -880,13 +892,13 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             }
         }
     } else {
-        // a warp reads the lanes 32 (warp % 4) .. + 31; the two of a quarter share its columns
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        constexpr int BLOCKS = TILE == 256 ? 4 : 1;
-        const int warp_row = (int)rank * ROWS + 32 * (TILE == 256 ? q : q & 1), warp_column = half * (32 * BLOCKS) + (TILE == 256 ? 0 : 64 * (q >> 1));
+        // a warp reads the lanes 32 (warp % 4) .. + 31; those of a quarter share its columns
+        constexpr bool PRECISE = TILE == 128;
+        constexpr int BLOCKS = PRECISE ? 2 : 4;
+        const int q = warp & 3, share = (warp - FIRST_EPI) >> 2;
+        const int warp_row = (int)rank * ROWS + 32 * (PRECISE ? q & 1 : q), warp_column = share * (16 * BLOCKS) + (PRECISE ? 64 * (q >> 1) : 0);
         const uint32_t t_empty0 = map_to_rank(t_empty, 0);
-        float *st = reinterpret_cast<float *>(raw + (base - raw_s) + RING_BYTES) + (warp - 2) * 1024;
-        int out_turn = 0;
+        unsigned char *st = raw + (base - raw_s) + STAGES * STAGE + (warp - FIRST_EPI) * 4096;
         unsigned *told = nullptr;  // the counter that is still to be told of this warp's last task
         // The copies are written; with them and this warp's other stores the completion is told.  It waits for memory, so that it comes when
         // the next task's first loads are under way, unless there is no next task yet.
@@ -910,20 +922,20 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
             if (ring[slot].end) break;
             next_slot();
             const int r0 = ti * TILE + warp_row, first = tj * TILE + warp_column;
-            const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 31) / 32, BLOCKS) : 0;
+            const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 15) / 16, BLOCKS) : 0;
             const int acc = n_done & 1;
-            const size_t at = ((size_t)(r0 / 32) * t.blocks + first / 32) * 1024 + lane * 4;
-            float4 x[8], next[8];
+            auto place = [&](int b) { return ((size_t)(r0 / 32) * t.blocks + (first + 16 * b) / 32) * 1024 + ((first + 16 * b) & 16) * 32 + lane * 4; };
+            float4 x[4], next[4];
             float row = 0.f, next_column = 0.f;
             if (blocks > 0 && t.phase != MUON_GRAM) {
-                if (t.phase <= MUON_MUL) next_column = __ldcg(t.vec2 + first + lane);
-                load_block(t.src + at, next);
+                if (t.phase <= MUON_MUL) next_column = __ldcg(t.vec2 + first + (lane & 15));
+                load_block(t.src + place(0), next);
                 row = __ldcg(t.vec + r0 + lane);
             }
             if (t.phase == MUON_FINAL && a.to == MUON_TO_PARAMS) {  // the parameters' rows on their way to L2
                 const int rows = t.transposed ? t.width : t.m, cols = t.transposed ? t.m : t.width;
-                for (int b = 0; b < blocks; ++b) {
-                    const int r = (t.transposed ? first + 32 * b : r0) + lane, c = t.transposed ? r0 : first + 32 * b;
+                for (int b = 0; b < 16 * blocks; b += 32) {
+                    const int r = (t.transposed ? first + b : r0) + lane, c = t.transposed ? r0 : first + b;
                     if (r < rows) prefetch_l2(static_cast<const float *>(a.out[t.tensor]) + (size_t)r * cols + c);
                 }
             }
@@ -936,25 +948,35 @@ __global__ void __launch_bounds__(THREADS, 1) muon_products_kernel(MuonArgs a, c
 #pragma unroll 1
                 for (int b = 0; b < blocks; ++b) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = next[k];
+                    for (int k = 0; k < 4; ++k) x[k] = next[k];
                     const float column = next_column;
                     if (t.phase != MUON_GRAM && b + 1 < blocks) {
-                        load_block(t.src + at + (b + 1) * 1024, next);
-                        if (t.phase <= MUON_MUL) next_column = __ldcg(t.vec2 + first + 32 * (b + 1) + lane);
+                        load_block(t.src + place(b + 1), next);
+                        if (t.phase <= MUON_MUL) next_column = __ldcg(t.vec2 + first + 16 * (b + 1) + (lane & 15));
                     }
-                    use(BlockAt{t.src2 + at + b * 1024, t.dst + at + b * 1024, tmem + acc * 256 + half * (32 * BLOCKS) + 32 * b + ((uint32_t)(q * 32) << 16), r0, first + 32 * b, lane, column, st});
+                    use(BlockAt{place(b), tmem + acc * 256 + share * (16 * BLOCKS) + 16 * b + ((uint32_t)(q * 32) << 16), r0, first + 16 * b, b, lane, column, st});
                 }
             };
             if (t.phase == MUON_GRAM)
-                each_block([&](const BlockAt &b) { block_gram(a, t, b, out_turn); });
+                each_block([&](const BlockAt &b) { block_gram<PRECISE>(t, b); });
             else if (t.phase == MUON_POLY)
-                each_block([&](const BlockAt &b) { block_poly(a, t, b, out_turn, x, row); });
+                each_block([&](const BlockAt &b) { block_poly<PRECISE>(a, t, b, x, row); });
             else if (t.phase == MUON_MUL)
-                each_block([&](const BlockAt &b) { block_mul(a, t, b, out_turn, x, row); });
+                each_block([&](const BlockAt &b) { block_mul<PRECISE>(t, b, x, row); });
             else if (t.phase == MUON_UPDATE)
-                each_block([&](const BlockAt &b) { block_update(a, t, b, out_turn, x, row); });
+                each_block([&](const BlockAt &b) { block_update<PRECISE>(t, b, x, row); });
             else
-                each_block([&](const BlockAt &b) { block_final(a, t, b, x, row); });
+                each_block([&](const BlockAt &b) { block_final(a, t, b, x, row, b.number + 1 < blocks); });
+            if (blocks > 0 && t.phase != MUON_FINAL) {
+                // (pad rows and columns: the copy leaves out what lies outside the matrix)
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_2d(a.maps + (size_t)t.out * MUON_MAP_BYTES, first, r0, smem_u32(st));
+                    if (PRECISE) tma_store_2d(a.maps + (size_t)t.out_lo * MUON_MAP_BYTES, first, r0, smem_u32(st + 2048));
+                    tma_store_commit();
+                }
+            }
             tc_before();
             __syncwarp();
             if (lane == 0) arrive_cluster(t_empty0 + 8 * acc);
@@ -991,8 +1013,8 @@ cudaError_t launch_products(const MuonArgs &a, const MuonProduct *products, cons
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)workers * 2u);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = SMEM;
+    cfg.blockDim = dim3(Shape<TILE>::THREADS);
+    cfg.dynamicSmemBytes = Shape<TILE>::SMEM;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;

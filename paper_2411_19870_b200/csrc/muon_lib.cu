@@ -263,7 +263,7 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
                 const size_t begin = plan->tasks.size();
                 each_tile(ceil_div(t.m, side), ceil_div(t.width, side), t.phase < MUON_UPDATE,
                           [&](int i, int j) { plan->tasks.push_back(MuonTask{product, (short)i, (short)j}); });
-                completed[e] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(2 * MUON_EPI_WARPS);
+                completed[e] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(2 * muon_epilogue_warps(side));
             }
             most = std::max(most, plan->tasks.size() - step);
         }
@@ -351,12 +351,12 @@ bool encode_maps(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, int tile, 
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     const cuuint64_t flat[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, row[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t panel[2] = {64, (cuuint32_t)tile / 2}, block[2] = {32, 32};
+    const cuuint32_t panel[2] = {64, (cuuint32_t)tile / 2}, block[2] = {tile == 256 ? 64u : 32u, 32};
     // blocks of 64 columns as the last axis (pad columns are read: they only reach results outside the matrix)
     const cuuint64_t cut[3] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64)}, cut_stride[2] = {(cuuint64_t)ld * 2, 128};
     const cuuint32_t two[3] = {64, 64, 2};
     return make(map, 2, flat, row, panel, CU_TENSOR_MAP_SWIZZLE_128B) && make(map + MUON_MAP_MN, 3, cut, cut_stride, two, CU_TENSOR_MAP_SWIZZLE_128B) &&
-           make(map + MUON_MAP_OUT, 2, flat, row, block, CU_TENSOR_MAP_SWIZZLE_64B);
+           make(map + MUON_MAP_OUT, 2, flat, row, block, tile == 256 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 template <typename T>
