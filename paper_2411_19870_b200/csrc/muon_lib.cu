@@ -57,12 +57,17 @@ struct demo_muon_ctx {
     MuonTile *d_tiles = nullptr;
     MuonProduct *d_products = nullptr;
     MuonTask *d_tasks = nullptr;
-    unsigned *d_done = nullptr;  // [n_tensors] completions, the next task behind them; [n_tensors] pieces ready
+    unsigned *d_done = nullptr;  // [n_tensors] completions; [n_tensors] pieces ready; the next task of each kind of tile
     float2 *d_scales = nullptr;
     char *d_maps = nullptr;
     char *d_work = nullptr;
     double *d_partials = nullptr;
+    int side_partials = 0;  // where those of tiles of 128 begin
     int *d_status = nullptr;
+    // Where there are matrices of both kinds of tile, those of 128 go through the iterations beside the others, on a stream of the context's
+    // own, which the caller's stream waits for (a ragged set of five matrices of 512 and one of 147 rows: 510 us one after the other, XXX so).
+    cudaStream_t side_stream = nullptr;
+    cudaEvent_t fork = nullptr, join = nullptr;
     Tables tables[ENTRY_POINTS];
     float *d_momentum = nullptr;  // reconstructed momenta of demo_muon_decode_apply, from its first call
     size_t momentum_bytes = 0;
@@ -85,6 +90,9 @@ void release(demo_muon_ctx *c)
     cudaFree(c->d_partials);
     cudaFree(c->d_status);
     cudaFree(c->d_momentum);
+    if (c->fork) cudaEventDestroy(c->fork);
+    if (c->join) cudaEventDestroy(c->join);
+    if (c->side_stream) cudaStreamDestroy(c->side_stream);
     for (Tables &t : c->tables) {
         cudaFree((void *)t.d_in);
         cudaFree((void *)t.d_mom);
@@ -98,8 +106,8 @@ struct Plan {
     std::vector<MuonTile> tiles;
     std::vector<MuonProduct> products;
     std::vector<MuonTask> tasks;
-    size_t work = 0;
-    int pieces = 0;
+    size_t work[2] = {0, 0};  // of the groups of each kind of tile, 256 and 128
+    int pieces[2] = {0, 0};
 };
 
 // Workspace of one matrix from `at` on, as offsets (the base is added once it is known).  Returns its end.
@@ -316,8 +324,9 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
         if (pieces > (1LL << 31) - 1) return DEMO_ERR_UNSUPPORTED;
         g.n_mats = (int)(end - at);
         g.n_pieces = (int)pieces;
-        plan->work = std::max(plan->work, work);
-        plan->pieces = std::max(plan->pieces, g.n_pieces);
+        const int kind = g.tile == 128;
+        plan->work[kind] = std::max(plan->work[kind], work);
+        plan->pieces[kind] = std::max(plan->pieces[kind], g.n_pieces);
         g.pack_tiles = (long long)plan->tiles.size();
         for (size_t e = at; e < end; ++e)
             for (int i = 0; i < ceil_div(all[e].m, MUON_PACK_TILE); ++i)
@@ -382,18 +391,22 @@ demo_status build(demo_muon_ctx *c)
     }
     const size_t T = (size_t)c->n_tensors;
     bool ok = alloc(c, &c->d_mats, T * sizeof(MuonMat)) && alloc(c, &c->d_tiles, plan.tiles.size() * sizeof(MuonTile)) &&
-              alloc(c, &c->d_done, (2 * T + 1) * sizeof(unsigned)) &&
+              alloc(c, &c->d_done, (2 * T + 2) * sizeof(unsigned)) &&
               alloc(c, &c->d_scales, T * sizeof(float2)) &&
-              alloc(c, &c->d_maps, T * MUON_MAPS * MUON_MAP_BYTES) && alloc(c, &c->d_work, plan.work) &&
-              alloc(c, &c->d_partials, (size_t)plan.pieces * sizeof(double)) && alloc(c, &c->d_status, sizeof(int));
+              alloc(c, &c->d_maps, T * MUON_MAPS * MUON_MAP_BYTES) && alloc(c, &c->d_work, plan.work[0] + plan.work[1]) &&
+              alloc(c, &c->d_partials, (size_t)(plan.pieces[0] + plan.pieces[1]) * sizeof(double)) && alloc(c, &c->d_status, sizeof(int));
     for (Tables &t : c->tables) {
         ok = ok && alloc(c, (void **)&t.d_in, T * sizeof(void *)) && alloc(c, (void **)&t.d_mom, T * sizeof(void *)) && alloc(c, (void **)&t.d_out, T * sizeof(void *));
         t.in.assign(T, nullptr);
         t.mom.assign(T, nullptr);
         t.out.assign(T, nullptr);
     }
+    if (ok && plan.work[0] && plan.work[1])
+        ok = cudaStreamCreateWithFlags(&c->side_stream, cudaStreamNonBlocking) == cudaSuccess && cudaEventCreateWithFlags(&c->fork, cudaEventDisableTiming) == cudaSuccess &&
+             cudaEventCreateWithFlags(&c->join, cudaEventDisableTiming) == cudaSuccess;
     if (!ok) return DEMO_ERR_ALLOC;
-    for (MuonMat &m : plan.mats) rebase(m, c->d_work);
+    for (MuonMat &m : plan.mats) rebase(m, c->d_work + (tile_of(m) == 128 ? plan.work[0] : 0));
+    c->side_partials = plan.pieces[0];
     st = make_tasks(c, &plan);
     if (st != DEMO_OK) return st;
     if (!alloc(c, &c->d_products, plan.products.size() * sizeof(MuonProduct)) || !alloc(c, &c->d_tasks, plan.tasks.size() * sizeof(MuonTask))) return DEMO_ERR_ALLOC;
@@ -412,7 +425,7 @@ demo_status build(demo_muon_ctx *c)
          cudaMemcpy(c->d_products, plan.products.data(), plan.products.size() * sizeof(MuonProduct), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_tasks, plan.tasks.data(), plan.tasks.size() * sizeof(MuonTask), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice) == cudaSuccess &&
-         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess && cudaMemset(c->d_done, 0, (2 * T + 1) * sizeof(unsigned)) == cudaSuccess;
+         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess && cudaMemset(c->d_done, 0, (2 * T + 2) * sizeof(unsigned)) == cudaSuccess;
     return ok ? DEMO_OK : DEMO_ERR_CUDA;
 }
 
@@ -448,10 +461,8 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     a.in = t.d_in;
     a.mom = t.d_mom;
     a.out = t.d_out;
-    a.partials = c->d_partials;
     a.done = c->d_done;
-    a.next_task = c->d_done + c->n_tensors;
-    a.ready = a.next_task + 1;
+    a.ready = c->d_done + c->n_tensors;
     a.scales = c->d_scales;
     a.nesterov = g.nesterov;
     a.mu = g.momentum;
@@ -463,11 +474,25 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     a.c = g.coefficients[2];
     a.status = c->d_status;
     cudaError_t err = cudaSuccess;
-    for (const Group &grp : c->groups) {
-        if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, stream);
-        if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, c->launch, stream);
-        if (err == cudaSuccess) err = muon_launch_products(grp.tile, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, stream);
-        c->launches += 3;
+    const bool both = c->side_stream != nullptr;
+    if (both) {
+        err = cudaEventRecord(c->fork, stream);
+        if (err == cudaSuccess) err = cudaStreamWaitEvent(c->side_stream, c->fork, 0);
+    }
+    for (int kind = 1; kind >= 0; --kind)  // (the small matrices first: they take a few SMs, the others the rest)
+        for (const Group &grp : c->groups) {
+            if ((grp.tile == 128) != (kind == 1)) continue;
+            cudaStream_t on = both && kind ? c->side_stream : stream;
+            a.partials = c->d_partials + (kind ? c->side_partials : 0);
+            a.next_task = c->d_done + 2 * c->n_tensors + kind;
+            if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, on);
+            if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, c->launch, on);
+            if (err == cudaSuccess) err = muon_launch_products(grp.tile, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, on);
+            c->launches += 3;
+        }
+    if (both) {  // (also after a failure: a forked capture has to be joined)
+        const cudaError_t joined = cudaEventRecord(c->join, c->side_stream), waited = cudaStreamWaitEvent(stream, c->join, 0);
+        if (err == cudaSuccess) err = joined != cudaSuccess ? joined : waited;
     }
     if (err != cudaSuccess) {
         cudaGetLastError();
