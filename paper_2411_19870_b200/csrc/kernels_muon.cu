@@ -465,15 +465,15 @@ struct BlockAt {
 // The fp16 values of a block into the warp's part of shared memory, from where one copy writes all of them: rows of 128 bytes, the 16-byte
 // pieces of row r at piece ^ (r % 8), or, in tiles of 128, where there are two blocks and the lo parts behind the hi parts, rows of 64 bytes at
 // piece ^ (r / 2 % 4).
-template <bool PRECISE>
+template <int TILE, bool PRECISE>
 __device__ __forceinline__ void stage_halves(const BlockAt &b, const float (&v)[16])
 {
     uint32_t p[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) p[k] = pack2(v[2 * k], v[2 * k + 1]);
     auto put = [&](unsigned char *at) {
-        const int swap = PRECISE ? b.lane >> 1 & 3 : b.lane & 7, piece = 2 * b.number;
-        unsigned char *row = at + b.lane * (PRECISE ? 64 : 128);
+        const int swap = TILE == 256 ? b.lane & 7 : b.lane >> 1 & 3, piece = 2 * b.number;
+        unsigned char *row = at + b.lane * (TILE == 256 ? 128 : 64);
         *reinterpret_cast<uint4 *>(row + ((piece ^ swap) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
         *reinterpret_cast<uint4 *>(row + (((piece + 1) ^ swap) << 4)) = make_uint4(p[4], p[5], p[6], p[7]);
     };
@@ -504,7 +504,7 @@ __device__ __forceinline__ bool on_diagonal(const BlockAt &b) { return (b.r0 ^ b
 __device__ __forceinline__ bool has_own(const BlockAt &b) { return (unsigned)(b.r0 + b.lane - b.j0) < 16u; }
 
 // E = A off the diagonal, d on it.
-template <bool PRECISE>
+template <int TILE, bool PRECISE>
 __device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &b)
 {
     float v[16];
@@ -515,12 +515,12 @@ __device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &
         const float own = take_own(b, v);
         if (has_own(b)) __stcg(t.diag + b.r0 + b.lane, own * MUON_EF_INV);
     }
-    stage_halves<PRECISE>(b, v);
+    stage_halves<TILE, PRECISE>(b, v);
     store_block(t.dst + b.fp32, v);
 }
 
 // B = a + b A + c A^2
-template <bool PRECISE>
+template <int TILE, bool PRECISE>
 __device__ __forceinline__ void block_poly(const MuonArgs &a, const MuonProduct &t, const BlockAt &b, const float4 (&e)[4], float di)
 {
     float v[16];
@@ -532,12 +532,12 @@ __device__ __forceinline__ void block_poly(const MuonArgs &a, const MuonProduct 
     const float base = fmaf(a.c, di, a.b), scale = a.c * MUON_EF_INV;
 #pragma unroll
     for (int k = 0; k < 16; ++k) v[k] = fmaf(fmaf(a.c, __shfl_sync(0xffffffffu, b.column, k), base), part(e, k), scale * v[k]);  // (E's own diagonal is zero)
-    stage_halves<PRECISE>(b, v);
+    stage_halves<TILE, PRECISE>(b, v);
     if (t.dst) store_block(t.dst + b.fp32, v);
 }
 
 // P Q, of matrices that commute
-template <bool PRECISE>
+template <int TILE, bool PRECISE>
 __device__ __forceinline__ void block_mul(const MuonProduct &t, const BlockAt &b, const float4 (&e)[4], float di)
 {
     float v[16];
@@ -551,19 +551,19 @@ __device__ __forceinline__ void block_mul(const MuonProduct &t, const BlockAt &b
     }
 #pragma unroll
     for (int k = 0; k < 16; ++k) v[k] = fmaf(di, part(f, k), fmaf(part(e, k), __shfl_sync(0xffffffffu, b.column, k), v[k] * MUON_EF_INV));
-    stage_halves<PRECISE>(b, v);
+    stage_halves<TILE, PRECISE>(b, v);
     if (t.dst) store_block(t.dst + b.fp32, v);
 }
 
 // X <- B X
-template <bool PRECISE>
+template <int TILE, bool PRECISE>
 __device__ __forceinline__ void block_update(const MuonProduct &t, const BlockAt &b, const float4 (&x)[4], float di)
 {
     float v[16];
     tmem_ld16(b.tmem, v);
 #pragma unroll
     for (int k = 0; k < 16; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV);
-    stage_halves<PRECISE>(b, v);
+    stage_halves<TILE, PRECISE>(b, v);
     store_block(t.dst + b.fp32, v);
 }
 
@@ -649,7 +649,7 @@ struct alignas(16) RingEntry {
 // Symmetric matrices exist above the diagonal only: left of it a panel's operand is loaded from the rows above, as its transpose.
 // A worker's tile is TILE x TILE: 256, of which each CTA's tensor memory holds half the rows, or 128, for small matrices: of its 64 rows a CTA
 // then holds the left 64 columns in lanes 0 .. 63 and the right ones in lanes 64 .. 127.
-template <int TILE>
+template <int TILE, bool PRECISE>
 __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
 {
     const StreamOrder order(1);
@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 const MuonProduct &p = *reinterpret_cast<const MuonProduct *>(words);
                 if (t >= 0 && tk.product != last_product) {
                     last_product = tk.product;
-                    for (int lo = 0; lo < (p.parts > 1 ? 2 : 1); ++lo) {
+                    for (int lo = 0; lo < (PRECISE ? 2 : 1); ++lo) {
                         const char *l = a.maps + (size_t)(lo ? p.left_lo : p.left) * MUON_MAP_BYTES, *r = a.maps + (size_t)(lo ? p.right_lo : p.right) * MUON_MAP_BYTES;
                         tmap_acquire(l);
                         tmap_acquire(r);
@@ -794,7 +794,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
             ok = all_of(wait_local(r_full + 8 * slot, turn));
             if (!ok) break;
             const RingEntry &e = ring[slot];
-            const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = uniform(e.p.parts), ti = uniform(e.i), tj = uniform(e.j);
+            const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
             const char *hi = a.maps + (size_t)uniform(left_side ? e.p.left : e.p.right) * MUON_MAP_BYTES;
             const char *lo = a.maps + (size_t)uniform(left_side ? e.p.left_lo : e.p.right_lo) * MUON_MAP_BYTES;
             const int panel = (left_side ? ti : tj) * TILE, at = panel + (int)rank * ROWS;
@@ -836,7 +836,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 ok = all_of(wait_local(r_full + 8 * slot, turn));
                 if (!ok) break;
                 const RingEntry &e = ring[slot];
-                const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = uniform(e.p.parts), ti = uniform(e.i), tj = uniform(e.j);
+                const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
                 const int left_rows = kind == MUON_GRAM ? 0 : ti * TILE, right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? tj * TILE : 1 << 30;
                 __syncwarp();
                 if (one) arrive(r_empty + 8 * slot);
@@ -893,10 +893,9 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
         }
     } else {
         // a warp reads the lanes 32 (warp % 4) .. + 31; those of a quarter share its columns
-        constexpr bool PRECISE = TILE == 128;
-        constexpr int BLOCKS = PRECISE ? 2 : 4;
+        constexpr int BLOCKS = TILE == 256 ? 4 : 2;
         const int q = warp & 3, share = (warp - FIRST_EPI) >> 2;
-        const int warp_row = (int)rank * ROWS + 32 * (PRECISE ? q & 1 : q), warp_column = share * (16 * BLOCKS) + (PRECISE ? 64 * (q >> 1) : 0);
+        const int warp_row = (int)rank * ROWS + 32 * (TILE == 256 ? q : q & 1), warp_column = share * (16 * BLOCKS) + (TILE == 256 ? 0 : 64 * (q >> 1));
         const uint32_t t_empty0 = map_to_rank(t_empty, 0);
         unsigned char *st = raw + (base - raw_s) + STAGES * STAGE + (warp - FIRST_EPI) * 4096;
         unsigned *told = nullptr;  // the counter that is still to be told of this warp's last task
@@ -958,13 +957,13 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 }
             };
             if (t.phase == MUON_GRAM)
-                each_block([&](const BlockAt &b) { block_gram<PRECISE>(t, b); });
+                each_block([&](const BlockAt &b) { block_gram<TILE, PRECISE>(t, b); });
             else if (t.phase == MUON_POLY)
-                each_block([&](const BlockAt &b) { block_poly<PRECISE>(a, t, b, x, row); });
+                each_block([&](const BlockAt &b) { block_poly<TILE, PRECISE>(a, t, b, x, row); });
             else if (t.phase == MUON_MUL)
-                each_block([&](const BlockAt &b) { block_mul<PRECISE>(t, b, x, row); });
+                each_block([&](const BlockAt &b) { block_mul<TILE, PRECISE>(t, b, x, row); });
             else if (t.phase == MUON_UPDATE)
-                each_block([&](const BlockAt &b) { block_update<PRECISE>(t, b, x, row); });
+                each_block([&](const BlockAt &b) { block_update<TILE, PRECISE>(t, b, x, row); });
             else
                 each_block([&](const BlockAt &b) { block_final(a, t, b, x, row, b.number + 1 < blocks); });
             if (blocks > 0 && t.phase != MUON_FINAL) {
@@ -997,10 +996,10 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
     }
 }
 
-template <int TILE>
+template <int TILE, bool PRECISE>
 cudaError_t launch_products(const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
 {
-    const void *kernel = reinterpret_cast<const void *>(muon_products_kernel<TILE>);
+    const void *kernel = reinterpret_cast<const void *>(muon_products_kernel<TILE, PRECISE>);
     cudaError_t err = demo_allow_smem(dev, kernel);
     if (err != cudaSuccess) return err;
     MuonArgs args = a;
@@ -1037,7 +1036,9 @@ cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_til
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_pack_kernel), n_tiles, NORM_THREADS, 0, stream, params);
 }
 
-cudaError_t muon_launch_products(int tile, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
+cudaError_t muon_launch_products(int tile, bool precise, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
 {
-    return tile == 256 ? launch_products<256>(a, products, tasks, n_tasks, workers, dev, stream) : launch_products<128>(a, products, tasks, n_tasks, workers, dev, stream);
+    if (precise) return launch_products<128, true>(a, products, tasks, n_tasks, workers, dev, stream);
+    return tile == 256 ? launch_products<256, false>(a, products, tasks, n_tasks, workers, dev, stream)
+                       : launch_products<128, false>(a, products, tasks, n_tasks, workers, dev, stream);
 }

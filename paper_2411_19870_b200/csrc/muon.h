@@ -28,6 +28,8 @@ struct MuonMat {
     int ldx, lde;      // multiples of 64
     int transposed;    // 1: X is the tensor's transpose
     int precise;       // 1: products take the lo parts, too
+    int tile;          // side of the products' tiles
+    int twos;          // 1: two iterations in one
     int tensor;        // position in the caller's pointer arrays
     int piece_begin;   // its first piece of the norm in the group, and how many
     int n_pieces;
@@ -69,7 +71,7 @@ struct alignas(16) MuonProduct {  // what the tasks of one product of one matrix
     int phase, mat;
     unsigned need;
     int steps;               // of K = 64
-    int parts;               // 1: the product of the hi parts; 2: hi lo and lo hi, too
+    int unused;
     int left, right, out;    // tensor maps of the operands and of the result
     int left_lo, right_lo, out_lo;
     int blocks;              // of x32 / e32 in a row of them
@@ -112,8 +114,8 @@ struct MuonArgs {
 cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n_pieces, DemoLaunch &dev, cudaStream_t stream);
 // X = S u / (||u|| + eps), as hi + lo; clears the counters of the matrices [first_mat, first_mat + n_mats) and the next task.
 cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, DemoLaunch &dev, cudaStream_t stream);
-// All products, in tiles of 256 x 256 or 128 x 128, by pairs of CTAs.
-cudaError_t muon_launch_products(int tile, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
+// All products, by pairs of CTAs.  precise: tiles of 128, of hi and lo parts.
+cudaError_t muon_launch_products(int tile, bool precise, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
 // Warps of an epilogue; each is a completion of a task in both CTAs.  (Sixteen for tiles of 128, too: 256 x 512 116 us instead of 107; eight of
 // 32 columns for tiles of 256: the 300M-class layers 11.2 ms instead of 10.9.)
 constexpr int muon_epilogue_warps(int tile) { return tile == 256 ? 16 : 8; }

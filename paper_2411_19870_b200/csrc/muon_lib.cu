@@ -20,6 +20,7 @@ namespace {
 struct Group {
     int first_mat, n_mats, n_pieces;
     int tile;              // side of the tiles
+    bool precise;
     long long pack_tiles;  // first of its list
     int n_pack;
     long long tasks;
@@ -57,15 +58,14 @@ struct demo_muon_ctx {
     MuonTile *d_tiles = nullptr;
     MuonProduct *d_products = nullptr;
     MuonTask *d_tasks = nullptr;
-    unsigned *d_done = nullptr;  // [n_tensors] completions; [n_tensors] pieces ready; the next task of each kind of tile
+    unsigned *d_done = nullptr;  // [n_tensors] completions; [n_tensors] pieces ready; the next task of each kind
     float2 *d_scales = nullptr;
     char *d_maps = nullptr;
     char *d_work = nullptr;
     double *d_partials = nullptr;
-    int side_partials = 0;  // where those of tiles of 128 begin
+    int side_partials = 0;  // where those of the precise matrices begin
     int *d_status = nullptr;
-    // Where there are matrices of both kinds of tile, those of 128 go through the iterations beside the others, on a stream of the context's
-    // own, which the caller's stream waits for (a ragged set of five matrices of 512 and one of 147 rows: 510 us one after the other, XXX so).
+    // Where there are matrices of both kinds, the precise ones go through the iterations beside the others, on a stream of the context's own, which the caller's stream waits for (a ragged set of five matrices of 512 and one of 147 rows: 510 us one after the other, XXX so).
     cudaStream_t side_stream = nullptr;
     cudaEvent_t fork = nullptr, join = nullptr;
     Tables tables[ENTRY_POINTS];
@@ -106,7 +106,7 @@ struct Plan {
     std::vector<MuonTile> tiles;
     std::vector<MuonProduct> products;
     std::vector<MuonTask> tasks;
-    size_t work[2] = {0, 0};  // of the groups of each kind of tile, 256 and 128
+    size_t work[2] = {0, 0};  // of the groups of each kind, the precise ones last
     int pieces[2] = {0, 0};
 };
 
@@ -148,11 +148,6 @@ void rebase(MuonMat &m, char *base)
     }
 }
 
-int tile_of(const MuonMat &m) { return m.m > PRECISE_SIDE ? 256 : 128; }
-
-// Two iterations in one (kernels_muon.cu) take 3 r + 5 products of m^3 multiplications, one after the other 6 r + 2, r = n / m.
-bool in_twos(const MuonMat &m, int steps) { return !m.precise && steps >= 3 && 2LL * m.n >= 3LL * m.m; }
-
 int ceil_div(int v, int by) { return (v + by - 1) / by; }
 
 // Tiles (i, j) of a grid in bands of eight rows, so that those in work together share rows and columns.
@@ -176,7 +171,6 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
         const bool wide = phase >= MUON_UPDATE;
         t.phase = phase;
         t.steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
-        t.parts = m.precise ? 2 : 1;
         t.m = m.m;
         t.width = wide ? m.n : m.m;
         t.blocks = (wide ? m.ldx : m.lde) / 32;
@@ -221,7 +215,7 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
     };
     for (int k = 0; k < steps;) {
         // the first alone: [1, 2, 2] has a third of the error of [2, 2, 1] where the rank is low
-        const bool two = in_twos(m, steps) && k > 0 && k + 2 <= steps;
+        const bool two = m.twos && k > 0 && k + 2 <= steps;
         gram(0);
         multiply(MUON_POLY, 0, 0, 1, two);
         if (two) {
@@ -279,6 +273,52 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
     return (int)std::min(most, (size_t)workers);
 }
 
+// Sets the tile and the way of the iterations of every matrix.
+// Two iterations in one take 3 r + 5 products of m^3 multiplications, one after the other 6 r + 2, r = n / m, but are one product longer.
+// Tiles of 256 multiply fastest, those of 128 pass from one product to the next fastest.  Which counts for a set is estimated from both: its
+// tasks spread over the workers, and its longest chain of products.  (512 x 4608 four times and 7511 x 512: XXX.)
+void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
+{
+    const double workers = std::max(1, c->launch.sm_count / 2);
+    auto set = [&](MuonMat &m, int tile, bool twos) {
+        m.tile = m.precise ? 128 : tile;
+        m.twos = twos && !m.precise && c->cfg.steps >= 3 && 2LL * m.n >= 3LL * m.m;
+        m.symmetric = m.twos ? 3 : 2;
+    };
+    double best = 0;
+    int best_tile = 0;
+    bool best_twos = false;
+    for (const int tile : {256, 128})
+        for (const bool twos : {true, false}) {
+            // us: of a step of K, of a task beside its steps, from a product's last step to the next one's first
+            const double step = tile == 256 ? 0.28 : 0.18, task = tile == 256 ? 1.5 : 1.0, handover = tile == 256 ? 8.5 : 5.0;
+            double total = 0, chain = 0;
+            const MuonMat *last = nullptr;
+            double last_total = 0;
+            for (MuonMat &m : *all) {
+                if (m.precise) continue;
+                if (!last || last->m != m.m || last->n != m.n) {
+                    MuonMat probe = m;
+                    set(probe, tile, twos);
+                    double one = 0;
+                    last_total = 0;
+                    for (const MuonProduct &t : products_of(probe, c->cfg.steps)) {
+                        const double rows = ceil_div(t.m, tile), cols = ceil_div(t.width, tile);
+                        const double tiles = t.phase < MUON_UPDATE ? rows * (rows + 1) / 2 : rows * cols;
+                        last_total += tiles * (t.steps * step + task);
+                        one += std::ceil(tiles / workers) * (t.steps * step + task) + handover;
+                    }
+                    chain = std::max(chain, one);
+                    last = &m;
+                }
+                total += last_total;
+            }
+            const double time = std::max(total / workers, chain) + 0.3 * std::min(total / workers, chain);
+            if (!best_tile || time < best) best = time, best_tile = tile, best_twos = twos;
+        }
+    for (MuonMat &m : *all) set(m, best_tile, best_twos);
+}
+
 demo_status make_plan(demo_muon_ctx *c, Plan *plan)
 {
     std::vector<MuonMat> all((size_t)c->n_tensors);
@@ -292,7 +332,6 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
         m.ldx = (int)round_up(m.n, 64);
         m.lde = (int)round_up(m.m, 64);
         m.precise = m.m <= PRECISE_SIDE;
-        m.symmetric = in_twos(m, c->cfg.steps) ? 3 : 2;
         m.tensor = t;
         // X's elements are of order one once its singular values are: then neither hi nor lo leaves the normal range of fp16
         m.S = (float)std::exp2(std::floor(0.5 * std::log2((double)m.n)));
@@ -301,16 +340,18 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
                        : c->cfg.scale == DEMO_SCALE_ASPECT ? std::sqrt(std::max(1.0f, (float)rows / (float)cols))
                                                            : 1.0f;
     }
-    // groups hold matrices of one kind of tile
-    std::stable_sort(all.begin(), all.end(), [](const MuonMat &x, const MuonMat &y) { return tile_of(x) > tile_of(y); });
+    choose_shapes(c, &all);
+    // groups hold matrices of one kind
+    std::stable_sort(all.begin(), all.end(), [](const MuonMat &x, const MuonMat &y) { return x.precise < y.precise; });
     for (size_t at = 0; at < all.size();) {
         Group g;
         std::memset(&g, 0, sizeof(g));
         g.first_mat = (int)at;
-        g.tile = tile_of(all[at]);
+        g.tile = all[at].tile;
+        g.precise = all[at].precise != 0;
         long long elements = 0, pieces = 0;
         size_t work = 0, end = at;
-        for (; end < all.size() && tile_of(all[end]) == g.tile; ++end) {
+        for (; end < all.size() && (all[end].precise != 0) == g.precise; ++end) {
             MuonMat &m = all[end];
             const long long n = (long long)m.m * m.n;
             if (end > at && elements + n > GROUP_ELEMENTS) break;
@@ -324,7 +365,7 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
         if (pieces > (1LL << 31) - 1) return DEMO_ERR_UNSUPPORTED;
         g.n_mats = (int)(end - at);
         g.n_pieces = (int)pieces;
-        const int kind = g.tile == 128;
+        const int kind = g.precise;
         plan->work[kind] = std::max(plan->work[kind], work);
         plan->pieces[kind] = std::max(plan->pieces[kind], g.n_pieces);
         g.pack_tiles = (long long)plan->tiles.size();
@@ -405,7 +446,7 @@ demo_status build(demo_muon_ctx *c)
         ok = cudaStreamCreateWithFlags(&c->side_stream, cudaStreamNonBlocking) == cudaSuccess && cudaEventCreateWithFlags(&c->fork, cudaEventDisableTiming) == cudaSuccess &&
              cudaEventCreateWithFlags(&c->join, cudaEventDisableTiming) == cudaSuccess;
     if (!ok) return DEMO_ERR_ALLOC;
-    for (MuonMat &m : plan.mats) rebase(m, c->d_work + (tile_of(m) == 128 ? plan.work[0] : 0));
+    for (MuonMat &m : plan.mats) rebase(m, c->d_work + (m.precise ? plan.work[0] : 0));
     c->side_partials = plan.pieces[0];
     st = make_tasks(c, &plan);
     if (st != DEMO_OK) return st;
@@ -415,9 +456,9 @@ demo_status build(demo_muon_ctx *c)
     for (MuonMat &m : plan.mats) {
         CUtensorMap *p = &maps[(size_t)m.maps];
         for (int k = 0; k < 2; ++k)
-            ok = ok && encode_maps(encode, p + MUON_MAP_X + k, tile_of(m), m.xhi[k], m.n, m.m, m.ldx) && encode_maps(encode, p + MUON_MAP_XLO + k, tile_of(m), m.xlo[k], m.n, m.m, m.ldx);
+            ok = ok && encode_maps(encode, p + MUON_MAP_X + k, m.tile, m.xhi[k], m.n, m.m, m.ldx) && encode_maps(encode, p + MUON_MAP_XLO + k, m.tile, m.xlo[k], m.n, m.m, m.ldx);
         for (int k = 0; k < m.symmetric; ++k)
-            ok = ok && encode_maps(encode, p + MUON_MAP_E + k, tile_of(m), m.ehi[k], m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_ELO + k, tile_of(m), m.elo[k], m.m, m.m, m.lde);
+            ok = ok && encode_maps(encode, p + MUON_MAP_E + k, m.tile, m.ehi[k], m.m, m.m, m.lde) && encode_maps(encode, p + MUON_MAP_ELO + k, m.tile, m.elo[k], m.m, m.m, m.lde);
     }
     if (!ok) return DEMO_ERR_CUDA;
     ok = cudaMemcpy(c->d_mats, plan.mats.data(), T * sizeof(MuonMat), cudaMemcpyHostToDevice) == cudaSuccess &&
@@ -481,13 +522,13 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     }
     for (int kind = 1; kind >= 0; --kind)  // (the small matrices first: they take a few SMs, the others the rest)
         for (const Group &grp : c->groups) {
-            if ((grp.tile == 128) != (kind == 1)) continue;
+            if (grp.precise != (kind == 1)) continue;
             cudaStream_t on = both && kind ? c->side_stream : stream;
             a.partials = c->d_partials + (kind ? c->side_partials : 0);
             a.next_task = c->d_done + 2 * c->n_tensors + kind;
             if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, on);
             if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, c->launch, on);
-            if (err == cudaSuccess) err = muon_launch_products(grp.tile, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, on);
+            if (err == cudaSuccess) err = muon_launch_products(grp.tile, grp.precise, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, on);
             c->launches += 3;
         }
     if (both) {  // (also after a failure: a forked capture has to be joined)
