@@ -329,8 +329,8 @@ constexpr long long TASK_WAIT_CYCLES = 20000000000LL;  // ~10 s: what is waited 
 
 __device__ __forceinline__ bool wait_local(uint32_t bar, unsigned parity) { return mbar_wait_bounded(bar, parity, TASK_WAIT_CYCLES); }
 // One lane of a warp that runs converged.  The loading and the MMA warp loop with all their lanes and leave only the instructions themselves to
-// one: operands formed in divergent code cost each MMA and each copy 100 to 200 cycles on their way to uniform registers (a step of a 256 tile:
-// 581 cycles instead of XXX, of which the products take 512).
+// one: operands formed in divergent code cost each MMA and each copy 100 to 200 cycles on their way to uniform registers (a step of a 256 tile
+// 581 cycles instead of 512, which is what the products take; 256 x 512 159 us instead of 136).
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t p;

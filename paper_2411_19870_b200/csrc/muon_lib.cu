@@ -65,7 +65,8 @@ struct demo_muon_ctx {
     double *d_partials = nullptr;
     int side_partials = 0;  // where those of the precise matrices begin
     int *d_status = nullptr;
-    // Where there are matrices of both kinds, the precise ones go through the iterations beside the others, on a stream of the context's own, which the caller's stream waits for (a ragged set of five matrices of 512 and one of 147 rows: 510 us one after the other, XXX so).
+    // Where there are matrices of both kinds, the precise ones go through the iterations beside the others, on a stream of the context's own,
+    // which the caller's stream waits for (five matrices of 512 rows and one of 147: 444 us, one after the other 510).
     cudaStream_t side_stream = nullptr;
     cudaEvent_t fork = nullptr, join = nullptr;
     Tables tables[ENTRY_POINTS];
@@ -234,8 +235,8 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
 
 // The products of the matrices mats[0 .. n), `first` the index of the first.  Matrices go through the iterations in cohorts, product by product,
 // every product matrix by matrix: with two rounds of the workers' tasks in a cohort's symmetric products, a matrix's next product starts when its last
-// is done, and the X of a cohort of small matrices stays in L2.  Returns how many workers the tasks keep busy: more would take turns, and every one of
-// them would come with cold instruction caches (one 256 x 512: 70 workers 155 us, 8 XXX).
+// is done.  (24 layers of a 1024-wide decoder: rounds 2 or 3 11.4 ms, 1.5 12.0, 1 13.4, 0.5 19.4; and 11.6 in the order in which workers of a
+// model of the device would start the tasks, with as few matrices under way as that takes.)  Returns how many workers the tasks keep busy.
 int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int side, Plan *plan)
 {
     const int workers = std::max(1, c->launch.sm_count / 2);
@@ -275,8 +276,12 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
 
 // Sets the tile and the way of the iterations of every matrix.
 // Two iterations in one take 3 r + 5 products of m^3 multiplications, one after the other 6 r + 2, r = n / m, but are one product longer.
-// Tiles of 256 multiply fastest, those of 128 pass from one product to the next fastest.  Which counts for a set is estimated from both: its
-// tasks spread over the workers, and its longest chain of products.  (512 x 4608 four times and 7511 x 512: XXX.)
+// Tiles of 256 multiply fastest (twice the products for the bytes that a CTA loads), those of 128 pass from one product to the next fastest (5
+// us instead of 8.5).  Which counts for a set is estimated from both: its tasks spread over the workers, and its longest chain of products.
+// Measured, us, tiles of 256 / 128, one after the other and in twos where that is not the same:
+//   512 x 512 166 / 96; 1024 x 1024 207 / 128, four of them 228 / 213; 2048 x 2048 302 / 368; 4096 x 4096 1203 / 2175
+//   512 x 2048 200, 249 / 121, 128; 512 x 4608, five of them 353, 362 / 346, 282; 1024 x 4096, four of them 450, 446 / 606, 470;
+//   2048 x 8192 721, 636 / 995, 773
 void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
 {
     const double workers = std::max(1, c->launch.sm_count / 2);
