@@ -146,7 +146,7 @@ __device__ __forceinline__ uint32_t pack2(float x, float y)
 }
 
 // A tile of 64 x 64 elements of X.
-__global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, const MuonTile *tiles, int first_mat, int n_mats)
+__global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, const MuonTile *tiles, int first_mat, int n_mats, int arrived, int n_arrived)
 {
     const StreamOrder order(1);
     constexpr int T = MUON_PACK_TILE;
@@ -162,6 +162,7 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
     order.begin();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.next_task = 0;
     for (int k = blockIdx.x * NORM_THREADS + threadIdx.x; k < n_mats; k += gridDim.x * NORM_THREADS) a.done[first_mat + k] = 0;
+    for (int k = blockIdx.x * NORM_THREADS + threadIdx.x; k < n_arrived; k += gridDim.x * NORM_THREADS) a.arrived[arrived + k] = 0;
     const void *in = a.in[mat.tensor];
     const float *mom = a.from == MUON_FROM_STEP ? a.mom[mat.tensor] : nullptr;
     float u[T / ROWS][4];
@@ -503,12 +504,10 @@ __device__ __forceinline__ float take_own(const BlockAt &b, float (&v)[16])
 __device__ __forceinline__ bool on_diagonal(const BlockAt &b) { return (b.r0 ^ b.j0) < 32; }  // (both below 2^31, multiples of 32 and 16)
 __device__ __forceinline__ bool has_own(const BlockAt &b) { return (unsigned)(b.r0 + b.lane - b.j0) < 16u; }
 
-// E = A off the diagonal, d on it.
+// E = A off the diagonal, d on it.  v: the products.
 template <int TILE, bool PRECISE>
-__device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &b)
+__device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &b, float (&v)[16])
 {
-    float v[16];
-    tmem_ld16(b.tmem, v);
 #pragma unroll
     for (int k = 0; k < 16; ++k) v[k] *= t.scale;
     if (on_diagonal(b)) {
@@ -517,6 +516,20 @@ __device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &
     }
     stage_halves<TILE, PRECISE>(b, v);
     store_block(t.dst + b.fp32, v);
+}
+
+// The parts of a sum, in their order.
+__device__ __forceinline__ void add_parts(const float *p, int n, size_t stride, float (&v)[16])
+{
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = 0.f;
+#pragma unroll 2
+    for (int s = 0; s < n; ++s) {
+        float4 x[4];
+        load_block(p + (size_t)s * stride, x);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] += part(x, k);
+    }
 }
 
 // B = a + b A + c A^2
@@ -637,7 +650,7 @@ __device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence
 
 struct alignas(16) RingEntry {
     MuonProduct p;
-    int i, j, end, pad;
+    int i, j, end, part, k0, steps, pad[2];  // part: of a sum over K, from step k0 on
 };
 
 // All products of all iterations, by persistent workers, pairs of CTAs.  Tasks are drawn in the list's order from one counter, so
@@ -723,7 +736,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     t = *static_cast<volatile int *>(drawn_ring + slot);
                     arrive_cluster(map_to_rank(q_empty + 8 * slot, 0));
                 }
-                MuonTask tk{0, 0, 0};
+                MuonTask tk{0, 0, 0, 0};
                 if (t >= 0) tk = tasks[t];
                 uint4 words[8];
                 {
@@ -760,7 +773,8 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     uint4 *to = reinterpret_cast<uint4 *>(ring + slot);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) to[k] = words[k];
-                    to[8] = make_uint4((unsigned)(int)tk.i, (unsigned)(int)tk.j, t < 0 ? 1u : 0u, 0u);
+                    to[8] = make_uint4((unsigned)(int)tk.i, (unsigned)(int)tk.j, t < 0 ? 1u : 0u, (unsigned)tk.part);
+                    to[9] = make_uint4((unsigned)(tk.part * p.steps), (unsigned)(tk.part == p.splits - 1 ? p.last_steps : p.steps), 0u, 0u);
                 }
                 arrive(r_full + 8 * slot);
                 next_slot();
@@ -794,9 +808,10 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
             ok = all_of(wait_local(r_full + 8 * slot, turn));
             if (!ok) break;
             const RingEntry &e = ring[slot];
-            const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
+            const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
             const char *hi = a.maps + (size_t)uniform(left_side ? e.p.left : e.p.right) * MUON_MAP_BYTES;
             const char *lo = a.maps + (size_t)uniform(left_side ? e.p.left_lo : e.p.right_lo) * MUON_MAP_BYTES;
+            const int k0 = uniform(e.k0);
             const int panel = (left_side ? ti : tj) * TILE, at = panel + (int)rank * ROWS;
             // from here on K's elements lie in the panel's rows
             const int rows_from = kind == MUON_GRAM ? 0 : left_side || kind <= MUON_MUL ? panel : 1 << 30;
@@ -813,7 +828,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     if (!ok) break;
                     if (one) {
                         if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * OPERAND);
-                        load_operand<ROWS>(base + stage * STAGE + (left_side ? 0 : OPERAND), part ? lo : hi, 64 * k < rows_from, at, 64 * k, full0 + 8 * stage);
+                        load_operand<ROWS>(base + stage * STAGE + (left_side ? 0 : OPERAND), part ? lo : hi, 64 * k < rows_from, at, 64 * (k0 + k), full0 + 8 * stage);
                     }
                     ++used;
                     if (++stage == STAGES) stage = 0, phase ^= 1;
@@ -836,7 +851,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 ok = all_of(wait_local(r_full + 8 * slot, turn));
                 if (!ok) break;
                 const RingEntry &e = ring[slot];
-                const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.p.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
+                const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
                 const int left_rows = kind == MUON_GRAM ? 0 : ti * TILE, right_rows = kind == MUON_GRAM ? 0 : kind <= MUON_MUL ? tj * TILE : 1 << 30;
                 __syncwarp();
                 if (one) arrive(r_empty + 8 * slot);
@@ -917,11 +932,11 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
             if (!ok) break;
             const MuonProduct &t = ring[slot].p;  // (the slot is free again when the task is done)
             const uint32_t slot_empty = r_empty + 8 * slot;
-            const int ti = ring[slot].i, tj = ring[slot].j;
+            const int ti = ring[slot].i, tj = ring[slot].j, part_no = ring[slot].part;
             if (ring[slot].end) break;
             next_slot();
             const int r0 = ti * TILE + warp_row, first = tj * TILE + warp_column;
-            const int blocks = r0 < t.m && first < t.width ? min((t.width - first + 15) / 16, BLOCKS) : 0;
+            int blocks = r0 < t.m && first < t.width ? min((t.width - first + 15) / 16, BLOCKS) : 0;
             const int acc = n_done & 1;
             auto place = [&](int b) { return ((size_t)(r0 / 32) * t.blocks + (first + 16 * b) / 32) * 1024 + ((first + 16 * b) & 16) * 32 + lane * 4; };
             float4 x[4], next[4];
@@ -943,6 +958,33 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_after();
+            // A part of a sum over K goes to memory; the warp whose part is the last to come adds all of them up, in their order, and goes on.
+            // (Sums in pieces are also the more exact: tensor cores truncate, 2^-24 of the sum for every 16 elements in one direction, and the
+            // diagonal of 1 x 2^20 came out 0.4 % small.)
+            constexpr size_t part_stride = (size_t)TILE * TILE;
+            const float *parts = nullptr;
+            bool mine = true;  // the task's results are this warp's to write
+            if (t.phase == MUON_GRAM && t.splits > 1) {
+                const int tile = tj * (tj + 1) / 2 + ti, place = ((int)rank * EPI_WARPS + warp - FIRST_EPI);
+                float *all = const_cast<float *>(t.src2) + (size_t)tile * t.splits * part_stride + (size_t)place * (BLOCKS * 512) + lane * 4;
+                parts = all;
+                for (int b = 0; b < blocks; ++b) {
+                    float v[16];
+                    tmem_ld16(tmem + acc * 256 + share * (16 * BLOCKS) + 16 * b + ((uint32_t)(q * 32) << 16), v);
+                    store_block(all + (size_t)part_no * part_stride + b * 512, v);
+                }
+                __syncwarp();
+                unsigned before = 0;
+                if (lane == 0) {
+                    unsigned *count = a.arrived + t.arrived + tile * (2 * EPI_WARPS) + place;
+                    __threadfence();
+                    before = atomicAdd(count, 1u);
+                    __threadfence();
+                    if (before == (unsigned)t.splits - 1u) atomicExch(count, 0u);  // for the next iteration
+                }
+                mine = __shfl_sync(0xffffffffu, before, 0) == (unsigned)t.splits - 1u;
+                if (!mine) blocks = 0;
+            }
             auto each_block = [&](auto use) {
 #pragma unroll 1
                 for (int b = 0; b < blocks; ++b) {
@@ -957,7 +999,15 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 }
             };
             if (t.phase == MUON_GRAM)
-                each_block([&](const BlockAt &b) { block_gram<TILE, PRECISE>(t, b); });
+                each_block([&](const BlockAt &b) {
+                    float v[16];
+                    if (t.splits == 1) {
+                        tmem_ld16(b.tmem, v);
+                    } else {
+                        add_parts(parts + b.number * 512, t.splits, part_stride, v);
+                    }
+                    block_gram<TILE, PRECISE>(t, b, v);
+                });
             else if (t.phase == MUON_POLY)
                 each_block([&](const BlockAt &b) { block_poly<TILE, PRECISE>(a, t, b, x, row); });
             else if (t.phase == MUON_MUL)
@@ -979,7 +1029,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
             tc_before();
             __syncwarp();
             if (lane == 0) arrive_cluster(t_empty0 + 8 * acc);
-            if (t.phase != MUON_FINAL) told = a.done + t.mat;
+            if (t.phase != MUON_FINAL && mine) told = a.done + t.mat;
             __syncwarp();
             if (lane == 0) arrive(slot_empty);
         }
@@ -1029,10 +1079,11 @@ cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_norm_kernel), n_pieces, NORM_THREADS, 0, stream, params);
 }
 
-cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, DemoLaunch &, cudaStream_t stream)
+cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, int arrived, int n_arrived, DemoLaunch &,
+                             cudaStream_t stream)
 {
     MuonArgs args = a;
-    void *params[] = {&args, &tiles, &first_mat, &n_mats};
+    void *params[] = {&args, &tiles, &first_mat, &n_mats, &arrived, &n_arrived};
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_pack_kernel), n_tiles, NORM_THREADS, 0, stream, params);
 }
 

@@ -40,6 +40,10 @@ struct MuonMat {
     uint16_t *xhi[2], *xlo[2];
     uint16_t *ehi[MUON_SYMMETRIC], *elo[MUON_SYMMETRIC];
     float *x32, *e32[MUON_SYMMETRIC], *diag[MUON_SYMMETRIC];
+    // GRAM's sum over K is cut into `splits` parts of `split_steps` steps, which lie in `parts` until the last of them adds them up
+    int splits, split_steps;
+    int arrived;       // index of its first counter: one for each tile, CTA and warp of the epilogue
+    float *parts;
 };
 // Tensor maps of a matrix (X twice, its lo parts, the symmetric matrices, theirs), three of each: boxes of 128 rows x 64 columns (an operand
 // whose rows run along K), two of 64 x 64 side by side (one whose columns do) and 32 x 64 (what an epilogue's warp writes), with 128-byte
@@ -66,25 +70,27 @@ enum { MUON_GRAM = 0, MUON_POLY = 1, MUON_MUL = 2, MUON_UPDATE = 3, MUON_FINAL =
 struct MuonTask {
     int product;
     short i, j;
+    int part;
 };
 struct alignas(16) MuonProduct {  // what the tasks of one product of one matrix share
     int phase, mat;
     unsigned need;
     int steps;               // of K = 64
-    int unused;
+    int splits;              // GRAM: parts of the sum over K; `steps` are a part's
     int left, right, out;    // tensor maps of the operands and of the result
     int left_lo, right_lo, out_lo;
     int blocks;              // of x32 / e32 in a row of them
     int m, width;            // of the result
     int tensor, transposed;
     const float *src;        // fp32: POLY, MUL: the left factor; UPDATE, FINAL: X
-    const float *src2;       // MUL: the right factor
+    const float *src2;       // MUL: the right factor; GRAM: the parts
     float *dst;              // fp32 result, NULL: not needed
     const float *vec;        // POLY, MUL: the left factor's diagonal; UPDATE, FINAL: the polynomial's
     const float *vec2;       // MUL: the right factor's diagonal
     float *diag;             // the result's diagonal
     float scale, step_scale; // GRAM: of A off the diagonal; FINAL: of O, of the update
-    int pad[2];
+    int last_steps;          // the last part's
+    int arrived;             // GRAM: see MuonMat; tile (i, j)'s are those of tile j (j + 1) / 2 + i
 };
 static_assert(sizeof(MuonProduct) == 128, "read as eight 16-byte pieces");
 
@@ -102,6 +108,7 @@ struct MuonArgs {
     float2 *scales;        // device: of each matrix, S / (||u|| + eps) in two factors
     unsigned *done;        // device: completions of each matrix's tasks
     unsigned *next_task;   // device
+    unsigned *arrived;     // device: parts of a sum that are there
     int from, to;
     int in_bf16, out_bf16;
     int nesterov;
@@ -112,8 +119,10 @@ struct MuonArgs {
 
 // Momentum update and the pieces' sums of squares; pieces [0, n_pieces) of the matrices [first, first + n).
 cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n_pieces, DemoLaunch &dev, cudaStream_t stream);
-// X = S u / (||u|| + eps), as hi + lo; clears the counters of the matrices [first_mat, first_mat + n_mats) and the next task.
-cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, DemoLaunch &dev, cudaStream_t stream);
+// X = S u / (||u|| + eps), as hi + lo; clears the counters of the matrices [first_mat, first_mat + n_mats), n_arrived of their parts' from
+// `arrived` on, and the next task.
+cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, int arrived, int n_arrived, DemoLaunch &dev,
+                             cudaStream_t stream);
 // All products, by pairs of CTAs.  precise: tiles of 128, of hi and lo parts.
 cudaError_t muon_launch_products(int tile, bool precise, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
 // Warps of an epilogue; each is a completion of a task in both CTAs.  (Sixteen for tiles of 128, too: 256 x 512 116 us instead of 107; eight of

@@ -25,6 +25,7 @@ struct Group {
     int n_pack;
     long long tasks;
     int n_tasks, workers;
+    int arrived, n_arrived;  // counters of the parts of its sums
 };
 
 // Pointer arrays of an entry point: device table and mirror, uploaded when they change.
@@ -60,6 +61,7 @@ struct demo_muon_ctx {
     MuonTask *d_tasks = nullptr;
     unsigned *d_done = nullptr;  // [n_tensors] completions; [n_tensors] pieces ready; the next task of each kind
     float2 *d_scales = nullptr;
+    unsigned *d_arrived = nullptr;
     char *d_maps = nullptr;
     char *d_work = nullptr;
     double *d_partials = nullptr;
@@ -86,6 +88,7 @@ void release(demo_muon_ctx *c)
     cudaFree(c->d_tasks);
     cudaFree(c->d_done);
     cudaFree(c->d_scales);
+    cudaFree(c->d_arrived);
     cudaFree(c->d_maps);
     cudaFree(c->d_work);
     cudaFree(c->d_partials);
@@ -109,7 +112,17 @@ struct Plan {
     std::vector<MuonTask> tasks;
     size_t work[2] = {0, 0};  // of the groups of each kind, the precise ones last
     int pieces[2] = {0, 0};
+    size_t arrived = 0;
 };
+
+int ceil_div(int v, int by) { return (v + by - 1) / by; }
+
+// Tiles of a symmetric product.
+int tiles_above(const MuonMat &m)
+{
+    const int k = ceil_div(m.m, m.tile);
+    return k * (k + 1) / 2;
+}
 
 // Workspace of one matrix from `at` on, as offsets (the base is added once it is known).  Returns its end.
 size_t place(MuonMat &m, size_t at)
@@ -125,6 +138,7 @@ size_t place(MuonMat &m, size_t at)
         m.xlo[p] = m.precise ? take(x) : m.xhi[p];
     }
     m.x32 = reinterpret_cast<float *>(take(rows * (size_t)m.ldx * 4));
+    m.parts = reinterpret_cast<float *>(m.splits > 1 ? reinterpret_cast<size_t>(take((size_t)m.splits * (size_t)tiles_above(m) * (size_t)(m.tile * m.tile) * 4)) : 0);
     for (int k = 0; k < m.symmetric; ++k) {
         m.ehi[k] = take(e);
         m.elo[k] = m.precise ? take(e) : m.ehi[k];
@@ -141,6 +155,7 @@ void rebase(MuonMat &m, char *base)
         move(m.xlo[p]);
     }
     move(m.x32);
+    move(m.parts);
     for (int k = 0; k < m.symmetric; ++k) {
         move(m.ehi[k]);
         move(m.elo[k]);
@@ -148,8 +163,6 @@ void rebase(MuonMat &m, char *base)
         move(m.diag[k]);
     }
 }
-
-int ceil_div(int v, int by) { return (v + by - 1) / by; }
 
 // Tiles (i, j) of a grid in bands of eight rows, so that those in work together share rows and columns.
 template <class Use>
@@ -171,7 +184,15 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
         std::memset(&t, 0, sizeof(t));
         const bool wide = phase >= MUON_UPDATE;
         t.phase = phase;
-        t.steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
+        t.steps = t.last_steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
+        t.splits = 1;
+        if (phase == MUON_GRAM && m.splits > 1) {
+            t.last_steps = t.steps - (m.splits - 1) * m.split_steps;
+            t.steps = m.split_steps;
+            t.splits = m.splits;
+            t.arrived = m.arrived;
+            t.src2 = m.parts;
+        }
         t.m = m.m;
         t.width = wide ? m.n : m.m;
         t.blocks = (wide ? m.ldx : m.lde) / 32;
@@ -264,9 +285,10 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
                 const int product = (int)plan->products.size();
                 plan->products.push_back(t);
                 const size_t begin = plan->tasks.size();
-                each_tile(ceil_div(t.m, side), ceil_div(t.width, side), t.phase < MUON_UPDATE,
-                          [&](int i, int j) { plan->tasks.push_back(MuonTask{product, (short)i, (short)j}); });
-                completed[e] += (unsigned)(plan->tasks.size() - begin) * (unsigned)(2 * muon_epilogue_warps(side));
+                each_tile(ceil_div(t.m, side), ceil_div(t.width, side), t.phase < MUON_UPDATE, [&](int i, int j) {
+                    for (int part = 0; part < t.splits; ++part) plan->tasks.push_back(MuonTask{product, (short)i, (short)j, part});
+                });
+                completed[e] += (unsigned)((plan->tasks.size() - begin) / (size_t)t.splits) * (unsigned)(2 * muon_epilogue_warps(side));
             }
             most = std::max(most, plan->tasks.size() - step);
         }
@@ -285,10 +307,27 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
 void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
 {
     const double workers = std::max(1, c->launch.sm_count / 2);
-    auto set = [&](MuonMat &m, int tile, bool twos) {
+    // tiles: of the symmetric products of all matrices of this kind
+    auto set = [&](MuonMat &m, int tile, bool twos, double tiles) {
         m.tile = m.precise ? 128 : tile;
         m.twos = twos && !m.precise && c->cfg.steps >= 3 && 2LL * m.n >= 3LL * m.m;
         m.symmetric = m.twos ? 3 : 2;
+        // Sums of up to 8192 elements (32768 where the products are of 11 bits) at a time for their exactness; and long ones in parts of 16 steps
+        // or more where three quarters of the workers have no tile (300 x 4000: 132 us instead of 143; with tiles for more of them the parts' way
+        // through memory costs what they save: 2048 x 8192 690 instead of 633).
+        const int steps = ceil_div(m.n, 64), exact = ceil_div(steps, m.precise ? 128 : 512);
+        const int spread = steps >= 48 && 4 * tiles <= workers ? std::min(steps / 16, (int)(workers / tiles)) : 1;
+        m.split_steps = ceil_div(steps, std::max(exact, spread));
+        m.splits = ceil_div(steps, m.split_steps);
+    };
+    auto all_tiles = [&](int tile, bool precise) {
+        double n = 0;
+        for (const MuonMat &m : *all)
+            if ((m.precise != 0) == precise) {
+                const double k = ceil_div(m.m, precise ? 128 : tile);
+                n += k * (k + 1) / 2;
+            }
+        return std::max(1.0, n);
     };
     double best = 0;
     int best_tile = 0;
@@ -298,20 +337,21 @@ void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
             // us: of a step of K, of a task beside its steps, from a product's last step to the next one's first
             const double step = tile == 256 ? 0.28 : 0.18, task = tile == 256 ? 1.5 : 1.0, handover = tile == 256 ? 8.5 : 5.0;
             double total = 0, chain = 0;
+            const double square = all_tiles(tile, false);
             const MuonMat *last = nullptr;
             double last_total = 0;
             for (MuonMat &m : *all) {
                 if (m.precise) continue;
                 if (!last || last->m != m.m || last->n != m.n) {
                     MuonMat probe = m;
-                    set(probe, tile, twos);
+                    set(probe, tile, twos, square);
                     double one = 0;
                     last_total = 0;
                     for (const MuonProduct &t : products_of(probe, c->cfg.steps)) {
                         const double rows = ceil_div(t.m, tile), cols = ceil_div(t.width, tile);
-                        const double tiles = t.phase < MUON_UPDATE ? rows * (rows + 1) / 2 : rows * cols;
+                        const double tiles = (t.phase < MUON_UPDATE ? rows * (rows + 1) / 2 : rows * cols) * t.splits;
                         last_total += tiles * (t.steps * step + task);
-                        one += std::ceil(tiles / workers) * (t.steps * step + task) + handover;
+                        one += std::ceil(tiles / workers) * (t.steps * step + task) + handover + (t.splits > 1 ? 2 : 0);
                     }
                     chain = std::max(chain, one);
                     last = &m;
@@ -321,7 +361,8 @@ void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
             const double time = std::max(total / workers, chain) + 0.3 * std::min(total / workers, chain);
             if (!best_tile || time < best) best = time, best_tile = tile, best_twos = twos;
         }
-    for (MuonMat &m : *all) set(m, best_tile, best_twos);
+    const double squares[2] = {all_tiles(best_tile, false), all_tiles(best_tile, true)};
+    for (MuonMat &m : *all) set(m, best_tile, best_twos, squares[m.precise != 0]);
 }
 
 demo_status make_plan(demo_muon_ctx *c, Plan *plan)
@@ -355,7 +396,7 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
         g.tile = all[at].tile;
         g.precise = all[at].precise != 0;
         long long elements = 0, pieces = 0;
-        size_t work = 0, end = at;
+        size_t work = 0, end = at, counters = 0;
         for (; end < all.size() && (all[end].precise != 0) == g.precise; ++end) {
             MuonMat &m = all[end];
             const long long n = (long long)m.m * m.n;
@@ -366,9 +407,15 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
             pieces += m.n_pieces;
             work = place(m, work);
             m.maps = (int)end * MUON_MAPS;
+            m.arrived = (int)(plan->arrived + counters);
+            if (m.splits > 1) counters += (size_t)tiles_above(m) * (size_t)(2 * muon_epilogue_warps(m.tile));
         }
         if (pieces > (1LL << 31) - 1) return DEMO_ERR_UNSUPPORTED;
         g.n_mats = (int)(end - at);
+        g.arrived = (int)plan->arrived;
+        g.n_arrived = (int)counters;
+        plan->arrived += counters;
+        if (plan->arrived > (size_t)(1LL << 30)) return DEMO_ERR_UNSUPPORTED;
         g.n_pieces = (int)pieces;
         const int kind = g.precise;
         plan->work[kind] = std::max(plan->work[kind], work);
@@ -438,7 +485,7 @@ demo_status build(demo_muon_ctx *c)
     const size_t T = (size_t)c->n_tensors;
     bool ok = alloc(c, &c->d_mats, T * sizeof(MuonMat)) && alloc(c, &c->d_tiles, plan.tiles.size() * sizeof(MuonTile)) &&
               alloc(c, &c->d_done, (2 * T + 2) * sizeof(unsigned)) &&
-              alloc(c, &c->d_scales, T * sizeof(float2)) &&
+              alloc(c, &c->d_scales, T * sizeof(float2)) && alloc(c, &c->d_arrived, (plan.arrived + 1) * sizeof(unsigned)) &&
               alloc(c, &c->d_maps, T * MUON_MAPS * MUON_MAP_BYTES) && alloc(c, &c->d_work, plan.work[0] + plan.work[1]) &&
               alloc(c, &c->d_partials, (size_t)(plan.pieces[0] + plan.pieces[1]) * sizeof(double)) && alloc(c, &c->d_status, sizeof(int));
     for (Tables &t : c->tables) {
@@ -510,6 +557,7 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
     a.done = c->d_done;
     a.ready = c->d_done + c->n_tensors;
     a.scales = c->d_scales;
+    a.arrived = c->d_arrived;
     a.nesterov = g.nesterov;
     a.mu = g.momentum;
     a.eps = g.eps;
@@ -532,7 +580,7 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stre
             a.partials = c->d_partials + (kind ? c->side_partials : 0);
             a.next_task = c->d_done + 2 * c->n_tensors + kind;
             if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, on);
-            if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, c->launch, on);
+            if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, grp.arrived, grp.n_arrived, c->launch, on);
             if (err == cudaSuccess) err = muon_launch_products(grp.tile, grp.precise, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, on);
             c->launches += 3;
         }
