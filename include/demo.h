@@ -352,10 +352,12 @@ demo_status demo_set_momentum_domain(demo_ctx *ctx, int32_t domain);
  * update: the matrix with its singular values moved towards one by Newton-Schulz iterations,
  *     X = U / (||U||_F + eps);   steps times:  A = X X^T,  X <- a X + (b A + c A^2) X;   O(U) = X
  * (for a matrix with more rows than columns of its transpose).  A demo_muon_ctx belongs to a list of matrices, of any sizes from 1 x 1,
- * and owns the workspace of the iterations: a few matrices at a time, as many as fill the device.
+ * and owns the workspace of the iterations: up to 26 bytes an element of as many matrices as make 128 million elements (or of the largest
+ * one), which go through the iterations together; demo_muon_workspace_bytes tells.
  *
- * Accuracy: products of fp16 operands accumulated in fp32; the linear term keeps 22 bits and the diagonal of A stays fp32.  Against
- * 64 bits O has a relative error (Frobenius norm) of about 1e-3, 1e-5 where the smaller side is at most 256, also where U has low rank.
+ * Accuracy: products of fp16 operands accumulated in fp32; everything else, the linear term and the diagonals among it, in fp32.  Against
+ * 64 bits O has a relative error (Frobenius norm) of up to 1e-3, 1e-2 where U has a rank of a few only; 1e-5 where the smaller side is at
+ * most 256, whose products take 22 bits.  Sums over a longer side n add n 2^-27, at most 1e-4.
  * Coefficients under which singular values grow beyond about 3 in the iterations leave the range of fp16: unspecified values.  NaN or Inf in a
  * matrix make its own result unspecified and no other's; a matrix of zeros gives zeros.  Results do not depend on the order of
  * execution: the same call on the same data gives the same bits.
@@ -385,9 +387,10 @@ typedef struct {
 } demo_muon_config;
 #define DEMO_MUON_MAX_STEPS 64
 #define DEMO_MUON_MAX_EXTENT (1 << 20)
+#define DEMO_MUON_MAX_TENSORS (1 << 16)
 
 /* tensors: descriptors with ndim 2.  Errors: INVALID_ARG (nulls, n_tensors < 1, values not finite, steps, eps, scale), SHAPE (ndim,
- * extents outside 1 .. DEMO_MUON_MAX_EXTENT), UNSUPPORTED (dtype, more than 2^20 tensors or 2^31 tiles, no tensor-map encoder), ALLOC, CUDA. */
+ * extents outside 1 .. DEMO_MUON_MAX_EXTENT), UNSUPPORTED (dtype, too many tensors or tiles, no tensor-map encoder), ALLOC, CUDA. */
 demo_status demo_muon_init(demo_muon_ctx **out, const demo_muon_config *cfg, const demo_tensor_desc *tensors, int32_t n_tensors,
                            int32_t cuda_device);
 

@@ -341,6 +341,13 @@ class DemoTransform:
         return ctypes.c_void_p(int(getattr(stream, "cuda_stream", stream)))
 
     @staticmethod
+    def _stream_on(stream, device: int) -> int:
+        """The given stream's handle, or the current stream of ``device``, which need not be the current device."""
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(device)
+        return int(getattr(stream, "cuda_stream", stream))
+
+    @staticmethod
     def _raw_stream(stream):
         """The stream as csrc/calls.cpp takes it: None for the current one, else its handle."""
         return None if stream is None else int(getattr(stream, "cuda_stream", stream))
@@ -551,35 +558,35 @@ class MuonTransform:
                 raise ValueError("%s: expected fp32 or bf16 tensors" % what)
         a, b = inputs[0].dtype, outputs[0].dtype
         st = self._calls.orthogonalize(self._fn["demo_orthogonalize"], self._ctx.value or 0, self._layouts[a], inputs, _DTYPES[a],
-                                       self._layouts[b], outputs, _DTYPES[b], DemoTransform._raw_stream(stream))
+                                       self._layouts[b], outputs, _DTYPES[b], DemoTransform._stream_on(stream, self.device))
         if st is None:
             st = self.lib.demo_orthogonalize(self._ctx, _checked(inputs, self.shapes, a, self.device, "inputs"), _DTYPES[a],
                                              _checked(outputs, self.shapes, b, self.device, "outputs"), _DTYPES[b],
-                                             DemoTransform._stream(stream))
+                                             DemoTransform._stream_on(stream, self.device))
         if st != 0:
             raise DemoError(st, "demo_orthogonalize")
 
     def step(self, grads, momentum, params, stream=None) -> None:
         f32 = self._layouts[torch.float32]
         st = self._calls.muon_step(self._fn["demo_muon_step"], self._ctx.value or 0, self._layouts[self._grad], f32, grads, momentum, params,
-                                   DemoTransform._raw_stream(stream))
+                                   DemoTransform._stream_on(stream, self.device))
         if st is None:
             st = self.lib.demo_muon_step(self._ctx, _checked(grads, self.shapes, self._grad, self.device, "grads"),
                                          _checked(momentum, self.shapes, torch.float32, self.device, "momentum"),
-                                         _checked(params, self.shapes, torch.float32, self.device, "params"), DemoTransform._stream(stream))
+                                         _checked(params, self.shapes, torch.float32, self.device, "params"), DemoTransform._stream_on(stream, self.device))
         if st != 0:
             raise DemoError(st, "demo_muon_step")
 
     def decode_apply(self, demo: DemoTransform, payloads, params, stream=None) -> None:
         """``demo.decode_apply`` with orthogonalised updates of its matrices, which are those of this context; ``params``: all of ``demo``'s."""
         st = self._calls.muon_decode(self._fn["demo_muon_decode_apply"], self._ctx.value or 0, demo._ctx.value or 0, demo._payload_ok, payloads,
-                                     demo._f32[1], params, DemoTransform._raw_stream(stream))
+                                     demo._f32[1], params, DemoTransform._stream_on(stream, self.device))
         if st is None:
             payloads = list(payloads)
             demo._check_payloads(payloads)
             st = self.lib.demo_muon_decode_apply(self._ctx, demo._ctx, _ptr_array(_tensor_ptrs(payloads)), len(payloads),
                                                  _checked(params, demo.shapes, torch.float32, self.device, "params"),
-                                                 DemoTransform._stream(stream))
+                                                 DemoTransform._stream_on(stream, self.device))
         if st != 0:
             raise DemoError(st, "demo_muon_decode_apply")
 
@@ -597,7 +604,7 @@ class MuonTransform:
         return int(self.lib.demo_muon_launch_count(self._ctx))
 
     def device_status(self, stream=None) -> int:
-        return int(self.lib.demo_muon_device_status(self._ctx, DemoTransform._stream(stream)))
+        return int(self.lib.demo_muon_device_status(self._ctx, DemoTransform._stream_on(stream, self.device)))
 
     def close(self) -> None:
         if getattr(self, "_ctx", None) is not None and self._ctx.value:
@@ -635,14 +642,14 @@ class AdamwTransform:
         """``step``: int64 tensor of one element on the device, the number of steps made so far; this call adds one."""
         f32 = self._layouts[torch.float32]
         st = self._calls.adamw_step(self._fn["demo_adamw_step"], self._ctx.value or 0, self._layouts[self._grad], f32, grads, exp_avg, exp_avg_sq,
-                                    params, self._count, (step,), DemoTransform._raw_stream(stream))
+                                    params, self._count, (step,), DemoTransform._stream_on(stream, self.device))
         if st is None:
             if step.dtype != torch.int64 or step.numel() != 1 or not step.is_cuda or step.device.index != self.device:
                 raise ValueError("step: need an int64 tensor of one element on cuda:%d" % self.device)
             lists = [_checked(t, self.shapes, d, self.device, w) for t, d, w in (
                 (grads, self._grad, "grads"), (exp_avg, torch.float32, "exp_avg"), (exp_avg_sq, torch.float32, "exp_avg_sq"),
                 (params, torch.float32, "params"))]
-            st = self.lib.demo_adamw_step(self._ctx, *lists, ctypes.c_void_p(step.data_ptr()), DemoTransform._stream(stream))
+            st = self.lib.demo_adamw_step(self._ctx, *lists, ctypes.c_void_p(step.data_ptr()), DemoTransform._stream_on(stream, self.device))
         if st != 0:
             raise DemoError(st, "demo_adamw_step")
 

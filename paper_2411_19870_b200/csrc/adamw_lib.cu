@@ -1,6 +1,7 @@
 // Host side of demo_adamw_* in include/demo.h.
 #include <cmath>
 #include <cstring>
+#include <exception>
 #include <new>
 #include <vector>
 
@@ -82,7 +83,7 @@ demo_status demo_adamw_init(demo_adamw_ctx **out, const demo_adamw_config *cfg, 
     if (st == DEMO_OK) {
         try {
             st = build(c, numels);
-        } catch (const std::bad_alloc &) {
+        } catch (const std::exception &) {
             st = DEMO_ERR_ALLOC;
         }
     }

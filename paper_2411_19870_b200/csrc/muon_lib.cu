@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <exception>
 #include <new>
 #include <vector>
 
@@ -40,7 +41,7 @@ struct Tables {
 };
 enum { FROM_ORTHOGONALIZE = 0, FROM_STEP = 1, FROM_DECODE = 2, ENTRY_POINTS = 3 };
 
-constexpr long long GROUP_ELEMENTS = 256LL << 20;  // workspace: 8 bytes for each, and A and F beside them
+constexpr long long GROUP_ELEMENTS = 128LL << 20;  // workspace: 8 bytes for each, and up to 18 bytes for each of the square matrices beside X
 constexpr int PRECISE_SIDE = 256;                 // up to here the products take the lo parts, too (kernels_muon.cu)
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -142,7 +143,7 @@ size_t place(MuonMat &m, size_t at)
     for (int k = 0; k < m.symmetric; ++k) {
         m.ehi[k] = take(e);
         m.elo[k] = m.precise ? take(e) : m.ehi[k];
-        m.e32[k] = reinterpret_cast<float *>(take(rows * (size_t)m.lde * 4));
+        m.e32[k] = m.symmetric == 2 && k == 1 ? nullptr : reinterpret_cast<float *>(take(rows * (size_t)m.lde * 4));  // (B of one iteration: not needed)
         m.diag[k] = reinterpret_cast<float *>(take((size_t)m.lde * 4));
     }
     return at;
@@ -159,7 +160,7 @@ void rebase(MuonMat &m, char *base)
     for (int k = 0; k < m.symmetric; ++k) {
         move(m.ehi[k]);
         move(m.elo[k]);
-        move(m.e32[k]);
+        if (m.symmetric > 2 || k == 0) move(m.e32[k]);
         move(m.diag[k]);
     }
 }
@@ -615,7 +616,7 @@ demo_status demo_muon_init(demo_muon_ctx **out, const demo_muon_config *cfg, con
     if (cfg->steps < 1 || cfg->steps > DEMO_MUON_MAX_STEPS || cfg->eps < 0 || (cfg->nesterov != 0 && cfg->nesterov != 1)) return DEMO_ERR_INVALID_ARG;
     if (cfg->scale != DEMO_SCALE_NONE && cfg->scale != DEMO_SCALE_ASPECT && cfg->scale != DEMO_SCALE_RMS) return DEMO_ERR_INVALID_ARG;
     if (cfg->grad_dtype != DEMO_F32 && cfg->grad_dtype != DEMO_BF16) return DEMO_ERR_UNSUPPORTED;
-    if (n_tensors > (1 << 20)) return DEMO_ERR_UNSUPPORTED;
+    if (n_tensors > DEMO_MUON_MAX_TENSORS) return DEMO_ERR_UNSUPPORTED;
     for (int t = 0; t < n_tensors; ++t) {
         const demo_tensor_desc &d = tensors[t];
         if (d.ndim != 2) return DEMO_ERR_SHAPE;
@@ -640,7 +641,7 @@ demo_status demo_muon_init(demo_muon_ctx **out, const demo_muon_config *cfg, con
             c->n_tensors = n_tensors;
             c->descs.assign(tensors, tensors + n_tensors);
             st = build(c);
-        } catch (const std::bad_alloc &) {
+        } catch (const std::exception &) {  // (no memory, or a list longer than a vector can be)
             st = DEMO_ERR_ALLOC;
         }
     }
@@ -742,7 +743,7 @@ demo_status demo_muon_decode_apply(demo_muon_ctx *ctx, demo_ctx *demo, const voi
         a.from = MUON_FROM_INPUT;
         a.to = MUON_TO_PARAMS;
         return run(ctx, a, t, stream);
-    } catch (const std::bad_alloc &) {
+    } catch (const std::exception &) {
         return DEMO_ERR_ALLOC;
     }
 }
