@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_norm_kernel(MuonArgs a, int
     __shared__ double scratch[NORM_THREADS / 32];
     const int e = find_mat(a.mats, first_mat, n_mats, blockIdx.x);
     const MuonMat &mat = a.mats[e];
-    const long long n = (long long)mat.m * mat.n, at = (long long)(blockIdx.x - mat.piece_begin) * MUON_PIECE;
+    const long long n = (long long)mat.m * mat.n, at = (long long)(blockIdx.x - mat.piece_begin) * a.piece;
     order.begin();
     const void *in = a.in[mat.tensor];
     float *mom = a.from == MUON_FROM_STEP ? a.mom[mat.tensor] : nullptr;
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_norm_kernel(MuonArgs a, int
         }
         sum += (double)g * (double)g;
     };
-    const int len = (int)(n - at < MUON_PIECE ? n - at : MUON_PIECE);
+    const int len = (int)(n - at < a.piece ? n - at : a.piece);
 #pragma unroll 4
     for (int i = threadIdx.x * 4; i + 3 < len; i += NORM_THREADS * 4) {
         float g[4];

@@ -56,7 +56,6 @@ constexpr int MUON_MAP_BYTES = 128;
 // 96 rows: error 1.6e-4 without).  Entries of up to 255 remain possible: singular values up to about 3 within the iterations.
 constexpr float MUON_EF_SCALE = 256.f, MUON_EF_INV = 1.f / 256.f;
 
-constexpr int MUON_PIECE = 8192;     // elements of a piece of the norm
 constexpr int MUON_PACK_TILE = 64;   // side of the tiles in which X is laid out
 
 struct MuonTile {
@@ -109,6 +108,7 @@ struct MuonArgs {
     unsigned *done;        // device: completions of each matrix's tasks
     unsigned *next_task;   // device
     unsigned *arrived;     // device: parts of a sum that are there
+    int piece;             // elements of a piece of the norm
     int from, to;
     int in_bf16, out_bf16;
     int nesterov;
