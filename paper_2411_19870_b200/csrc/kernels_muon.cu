@@ -145,6 +145,22 @@ __device__ __forceinline__ uint32_t pack2(float x, float y)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// Tiles of 128 read pad columns along K: those of the other matrices of the workspace beside four elements (i, j ..) of X are set to zero.
+__device__ __forceinline__ void clear_pads(const MuonMat &mat, int i, int j)
+{
+    if (j + 4 > mat.n)
+        for (int l = max(j, mat.n); l < j + 4; ++l) {
+            mat.xhi[1][(size_t)i * mat.ldx + l] = 0;
+            mat.xlo[1][(size_t)i * mat.ldx + l] = 0;
+        }
+    if (j < 64)  // (sixteen threads a row)
+        for (int l = mat.m + j / 4; l < mat.lde; l += 16)
+            for (int e = 0; e < mat.symmetric; ++e) {
+                mat.ehi[e][(size_t)i * mat.lde + l] = 0;
+                mat.elo[e][(size_t)i * mat.lde + l] = 0;
+            }
+}
+
 // A tile of 64 x 64 elements of X.
 __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, const MuonTile *tiles, int first_mat, int n_mats, int arrived, int n_arrived)
 {
@@ -230,6 +246,7 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
 #pragma unroll
             for (int l = 0; l < 4; ++l) w[l] = tile[i][x + l];
             *reinterpret_cast<uint2 *>(mat.xhi[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
+            if (mat.tile == 128) clear_pads(mat, i0 + i, j0 + x);
             if (mat.precise) {
 #pragma unroll
                 for (int l = 0; l < 4; ++l) w[l] -= __half2float(__float2half_rn(w[l]));
@@ -253,8 +270,8 @@ constexpr int TMEM_COLS = 512;
 template <int TILE>
 struct Shape {
     static constexpr int EPI_WARPS = muon_epilogue_warps(TILE), THREADS = 32 * (FIRST_EPI + EPI_WARPS);
-    // a CTA's rows of both operands of a step of K = 64, as many steps as there is room for beside 4 KB for each warp of the epilogue
-    static constexpr int ROWS = TILE / 2, OPERAND = ROWS * 128, STAGE = 2 * OPERAND, STAGES = (224 * 1024 - EPI_WARPS * 4096) / STAGE;
+    // a CTA's rows of both operands of a step of K, as many steps as there is room for beside 4 KB for each warp of the epilogue
+    static constexpr int ROWS = TILE / 2, K = muon_k_step(TILE), OPERAND = ROWS * K * 2, STAGE = 2 * OPERAND, STAGES = (224 * 1024 - EPI_WARPS * 4096) / STAGE;
     static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * 4096 + 1024;
 };
 
@@ -295,8 +312,8 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// One operand of a step: rows of 64 elements (K-major), or, column by column, blocks of 64 rows of K (MN-major; two of them side by side come
-// as a third dimension).  The loads of both CTAs are counted by the barrier of the first.
+// One operand of a step (MUON_MAPS), one copy: a loading warp takes 340 cycles for one and what belongs to it, whatever its size.  The loads of
+// both CTAs are counted by the barrier of the first.
 __device__ __forceinline__ void load_2d(uint32_t dst, const void *map, int x, int y, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x),
@@ -309,15 +326,13 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const void *map, int x, in
                  "r"(y), "r"(x / 64), "r"(bar)
                  : "memory");
 }
-template <int ROWS>
+template <int TILE>
 __device__ __forceinline__ void load_operand(uint32_t dst, const char *map, bool columns, int at, int k, uint32_t bar)
 {
-    if (!columns)
-        load_2d(dst, map, k, at, bar);
-    else if (ROWS == 64)
-        load_2d(dst, map, at, k, bar);
+    if ((TILE == 256) != columns)
+        load_2d(dst, map, columns ? at : k, columns ? k : at, bar);
     else
-        load_3d(dst, map + MUON_MAP_MN * MUON_MAP_BYTES, at, k, bar);
+        load_3d(dst, map + MUON_MAP_TWO * MUON_MAP_BYTES, columns ? at : k, columns ? k : at, bar);
 }
 // (release at the scope of the CTA even where the barrier is another CTA's: one of the cluster's would wait for this warp's stores to memory)
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
@@ -666,8 +681,8 @@ template <int TILE, bool PRECISE>
 __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(MuonArgs a, const MuonProduct *products, const MuonTask *tasks, int n_tasks)
 {
     const StreamOrder order(1);
-    constexpr int ROWS = Shape<TILE>::ROWS, OPERAND = Shape<TILE>::OPERAND, STAGE = Shape<TILE>::STAGE, STAGES = Shape<TILE>::STAGES, EPI_WARPS = Shape<TILE>::EPI_WARPS;
-    constexpr int RING = 4, NEAR_STEPS = 8;
+    constexpr int ROWS = Shape<TILE>::ROWS, K = Shape<TILE>::K, OPERAND = Shape<TILE>::OPERAND, STAGE = Shape<TILE>::STAGE, STAGES = Shape<TILE>::STAGES, EPI_WARPS = Shape<TILE>::EPI_WARPS;
+    constexpr int RING = 4, NEAR_STEPS = 512 / K;
     extern __shared__ unsigned char raw[];
     __shared__ unsigned long long bars[2 * STAGES + 4 + 5 * RING + 2];
     __shared__ RingEntry ring[RING];
@@ -749,11 +764,13 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     last_product = tk.product;
                     for (int lo = 0; lo < (PRECISE ? 2 : 1); ++lo) {
                         const char *l = a.maps + (size_t)(lo ? p.left_lo : p.left) * MUON_MAP_BYTES, *r = a.maps + (size_t)(lo ? p.right_lo : p.right) * MUON_MAP_BYTES;
-                        tmap_acquire(l);
-                        tmap_acquire(r);
-                        if (TILE == 256 && p.phase != MUON_GRAM) {
-                            tmap_acquire(l + MUON_MAP_MN * MUON_MAP_BYTES);
-                            tmap_acquire(r + MUON_MAP_MN * MUON_MAP_BYTES);
+                        if (TILE == 256 || p.phase != MUON_GRAM) {
+                            tmap_acquire(l);
+                            tmap_acquire(r);
+                        }
+                        if (TILE == 128 || p.phase != MUON_GRAM) {
+                            tmap_acquire(l + MUON_MAP_TWO * MUON_MAP_BYTES);
+                            tmap_acquire(r + MUON_MAP_TWO * MUON_MAP_BYTES);
                         }
                         if (p.phase != MUON_FINAL) tmap_acquire(a.maps + (size_t)(lo ? p.out_lo : p.out) * MUON_MAP_BYTES);
                     }
@@ -828,7 +845,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     if (!ok) break;
                     if (one) {
                         if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * OPERAND);
-                        load_operand<ROWS>(base + stage * STAGE + (left_side ? 0 : OPERAND), part ? lo : hi, 64 * k < rows_from, at, 64 * (k0 + k), full0 + 8 * stage);
+                        load_operand<TILE>(base + stage * STAGE + (left_side ? 0 : OPERAND), part ? lo : hi, K * k < rows_from, at, K * (k0 + k), full0 + 8 * stage);
                     }
                     ++used;
                     if (++stage == STAGES) stage = 0, phase ^= 1;
@@ -862,16 +879,18 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 if (!ok) break;
                 tc_after();
                 const uint32_t d = tmem + acc * 256;
-                // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row.  MN-major: blocks of 64 columns
-                // 8192 bytes apart, groups of 8 rows of K 1024.
-                auto multiply = [&](uint64_t da, uint64_t db, uint32_t idesc, uint32_t a_step, uint32_t b_step, uint32_t accumulate) {
+                // K-major: groups of 8 rows 1024 bytes apart, 16 elements of K 32 bytes further in the row, the next 64 of K 8192 bytes further.
+                // MN-major: blocks of 64 columns 8192 bytes apart, groups of 8 rows of K 1024.
+                auto multiply = [&](uint64_t da, uint64_t db, uint32_t idesc, bool a_mn, bool b_mn, uint32_t accumulate) {
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) mma_f16(d, da + kk * a_step, db + kk * b_step, idesc, kk ? 1u : accumulate);
+                    for (int kk = 0; kk < K / 16; ++kk) {
+                        const uint32_t rows = (32 * (kk & 3) + 8192 * (kk >> 2)) >> 4, columns = (2048 * kk) >> 4;
+                        mma_f16(d, da + (a_mn ? columns : rows), db + (b_mn ? columns : rows), idesc, kk ? 1u : accumulate);
+                    }
                 };
                 for (int k = 0; k < steps; ++k) {
-                    const bool a_mn = 64 * k < left_rows, b_mn = 64 * k < right_rows;
+                    const bool a_mn = K * k < left_rows, b_mn = K * k < right_rows;
                     const uint32_t idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
-                    const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
                     const uint64_t a_at = operand_desc(0, a_mn ? 8192 : 16, 1024), b_at = operand_desc(0, b_mn ? 8192 : 16, 1024);
                     const uint32_t at = (base + stage * STAGE) >> 4;  // (below 2^14)
                     const uint64_t da = a_at + at, db = b_at + at + (OPERAND >> 4);
@@ -879,7 +898,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     if (!ok) break;
                     tc_after();
                     const int hi = stage;
-                    if (one) multiply(da, db, idesc, a_step, b_step, k ? 1u : 0u);
+                    if (one) multiply(da, db, idesc, a_mn, b_mn, k ? 1u : 0u);
                     if (++stage == STAGES) stage = 0, phase ^= 1;
                     if (parts > 1) {  // the next stage holds the lo parts
                         ok = all_of(wait_local(full + 8 * stage, phase));
@@ -887,8 +906,8 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                         tc_after();
                         const uint32_t at_lo = (base + stage * STAGE) >> 4;
                         if (one) {
-                            multiply(da, b_at + at_lo + (OPERAND >> 4), idesc, a_step, b_step, 1u);
-                            multiply(a_at + at_lo, db, idesc, a_step, b_step, 1u);
+                            multiply(da, b_at + at_lo + (OPERAND >> 4), idesc, a_mn, b_mn, 1u);
+                            multiply(a_at + at_lo, db, idesc, a_mn, b_mn, 1u);
                             mma_commit(empty + 8 * hi);
                             mma_commit(empty + 8 * stage);
                         }

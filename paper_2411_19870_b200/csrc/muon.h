@@ -45,11 +45,12 @@ struct MuonMat {
     int arrived;       // index of its first counter: one for each tile, CTA and warp of the epilogue
     float *parts;
 };
-// Tensor maps of a matrix (X twice, its lo parts, the symmetric matrices, theirs), three of each: boxes of 128 rows x 64 columns (an operand
-// whose rows run along K), two of 64 x 64 side by side (one whose columns do) and 32 x 64 (what an epilogue's warp writes), with 128-byte
-// swizzle; of matrices in tiles of 128, 64 x 64 for both operands and 32 x 32 with 64-byte swizzle.
+// Tensor maps of a matrix (X twice, its lo parts, the symmetric matrices, theirs), three of each: boxes of 128 rows x 64 columns, of two times
+// 64 x 64 side by side, both with 128-byte swizzle, and what an epilogue's warp writes: 32 x 64, or, in tiles of 128, 32 x 32 with 64-byte
+// swizzle.  An operand is, for tiles of 256, 128 rows by 64 of K: the first where its rows run along K, the second where its columns do; for
+// tiles of 128, 64 rows by 128 of K: the other way round.
 enum { MUON_MAP_X = 0, MUON_MAP_XLO = 2, MUON_MAP_E = 4, MUON_MAP_ELO = 4 + MUON_SYMMETRIC, MUON_MAP_KINDS = 4 + 2 * MUON_SYMMETRIC };
-constexpr int MUON_MAP_MN = MUON_MAP_KINDS, MUON_MAP_OUT = 2 * MUON_MAP_KINDS, MUON_MAPS = 3 * MUON_MAP_KINDS;
+constexpr int MUON_MAP_TWO = MUON_MAP_KINDS, MUON_MAP_OUT = 2 * MUON_MAP_KINDS, MUON_MAPS = 3 * MUON_MAP_KINDS;
 constexpr int MUON_MAP_BYTES = 128;
 
 // Off the diagonal, symmetric matrices lie in the workspace 256 times as large: entries of 1/m and less, and their lo parts, stay in fp16's normal range (of rank one,
@@ -74,7 +75,7 @@ struct MuonTask {
 struct alignas(16) MuonProduct {  // what the tasks of one product of one matrix share
     int phase, mat;
     unsigned need;
-    int steps;               // of K = 64
+    int steps;               // of muon_k_step(tile)
     int splits;              // GRAM: parts of the sum over K; `steps` are a part's
     int left, right, out;    // tensor maps of the operands and of the result
     int left_lo, right_lo, out_lo;
@@ -127,4 +128,5 @@ cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_til
 cudaError_t muon_launch_products(int tile, bool precise, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
 // Warps of an epilogue; each is a completion of a task in both CTAs.  (Sixteen for tiles of 128, too: 256 x 512 116 us instead of 107; eight of
 // 32 columns for tiles of 256: the 300M-class layers 11.2 ms instead of 10.9.)
+constexpr int muon_k_step(int tile) { return 16384 / tile; }
 constexpr int muon_epilogue_warps(int tile) { return tile == 256 ? 16 : 8; }

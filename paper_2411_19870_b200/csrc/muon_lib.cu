@@ -185,7 +185,7 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
         std::memset(&t, 0, sizeof(t));
         const bool wide = phase >= MUON_UPDATE;
         t.phase = phase;
-        t.steps = t.last_steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, 64);
+        t.steps = t.last_steps = ceil_div(phase == MUON_GRAM ? m.n : m.m, muon_k_step(m.tile));
         t.splits = 1;
         if (phase == MUON_GRAM && m.splits > 1) {
             t.last_steps = t.steps - (m.splits - 1) * m.split_steps;
@@ -313,11 +313,11 @@ void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
         m.tile = m.precise ? 128 : tile;
         m.twos = twos && !m.precise && c->cfg.steps >= 3 && 2LL * m.n >= 3LL * m.m;
         m.symmetric = m.twos ? 3 : 2;
-        // Sums of up to 8192 elements (32768 where the products are of 11 bits) at a time for their exactness; and long ones in parts of 16 steps
+        // Sums of up to 8192 elements (32768 where the products are of 11 bits) at a time for their exactness; and long ones in parts of 1024
         // or more where three quarters of the workers have no tile (300 x 4000: 132 us instead of 143; with tiles for more of them the parts' way
         // through memory costs what they save: 2048 x 8192 690 instead of 633).
-        const int steps = ceil_div(m.n, 64), exact = ceil_div(steps, m.precise ? 128 : 512);
-        const int spread = steps >= 48 && 4 * tiles <= workers ? std::min(steps / 16, (int)(workers / tiles)) : 1;
+        const int steps = ceil_div(m.n, muon_k_step(m.tile)), exact = ceil_div(m.n, m.precise ? 8192 : 32768);
+        const int spread = m.n >= 48 * 64 && 4 * tiles <= workers ? std::min(m.n / 1024, (int)(workers / tiles)) : 1;
         m.split_steps = ceil_div(steps, std::max(exact, spread));
         m.splits = ceil_div(steps, m.split_steps);
     };
@@ -336,7 +336,7 @@ void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
     for (const int tile : {256, 128})
         for (const bool twos : {true, false}) {
             // us: of a step of K, of a task beside its steps, from a product's last step to the next one's first
-            const double step = tile == 256 ? 0.28 : 0.18, task = tile == 256 ? 1.5 : 1.0, handover = tile == 256 ? 8.5 : 5.0;
+            const double step = tile == 256 ? 0.28 : 0.2, task = tile == 256 ? 1.5 : 1.0, handover = tile == 256 ? 8.5 : 5.0;
             double total = 0, chain = 0;
             const double square = all_tiles(tile, false);
             const MuonMat *last = nullptr;
@@ -464,11 +464,11 @@ bool encode_maps(PFN_cuTensorMapEncodeTiled encode, CUtensorMap *map, int tile, 
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     const cuuint64_t flat[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, row[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t panel[2] = {64, (cuuint32_t)tile / 2}, block[2] = {tile == 256 ? 64u : 32u, 32};
-    // blocks of 64 columns as the last axis (pad columns are read: they only reach results outside the matrix)
+    const cuuint32_t panel[2] = {64, 128}, block[2] = {tile == 256 ? 64u : 32u, 32};
+    // blocks of 64 columns as the last axis (pad columns are read: along K they are zero, else they only reach results outside the matrix)
     const cuuint64_t cut[3] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64)}, cut_stride[2] = {(cuuint64_t)ld * 2, 128};
     const cuuint32_t two[3] = {64, 64, 2};
-    return make(map, 2, flat, row, panel, CU_TENSOR_MAP_SWIZZLE_128B) && make(map + MUON_MAP_MN, 3, cut, cut_stride, two, CU_TENSOR_MAP_SWIZZLE_128B) &&
+    return make(map, 2, flat, row, panel, CU_TENSOR_MAP_SWIZZLE_128B) && make(map + MUON_MAP_TWO, 3, cut, cut_stride, two, CU_TENSOR_MAP_SWIZZLE_128B) &&
            make(map + MUON_MAP_OUT, 2, flat, row, block, tile == 256 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
