@@ -67,9 +67,10 @@ struct demo_muon_ctx {
     char *d_work = nullptr;
     double *d_partials = nullptr;
     int side_partials = 0;  // where those of the precise matrices begin
+    int side_workers = 0;   // workers of the precise matrices where there are others, too
     int *d_status = nullptr;
     // Where there are matrices of both kinds, the precise ones go through the iterations beside the others, on a stream of the context's own,
-    // which the caller's stream waits for (five matrices of 512 rows and one of 147: 444 us, one after the other 510).
+    // which the caller's stream waits for (five matrices of 512 rows and one of 147: 302 us, the five alone 293).
     cudaStream_t side_stream = nullptr;
     cudaEvent_t fork = nullptr, join = nullptr;
     Tables tables[ENTRY_POINTS];
@@ -261,7 +262,8 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
 // model of the device would start the tasks, with as few matrices under way as that takes.)  Returns how many workers the tasks keep busy.
 int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int side, Plan *plan)
 {
-    const int workers = std::max(1, c->launch.sm_count / 2);
+    const int device = std::max(1, c->launch.sm_count / 2);
+    const int workers = std::max(1, c->side_workers == 0 ? device : mats[0].precise ? c->side_workers : device - c->side_workers);
     auto symmetric = [&](const MuonMat &m) { const long long k = ceil_div(m.m, side); return k * (k + 1) / 2; };
     long long total = 0;
     for (int e = 0; e < n; ++e) total += symmetric(mats[e]);
@@ -305,7 +307,7 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
 //   512 x 512 166 / 96; 1024 x 1024 207 / 128, four of them 228 / 213; 2048 x 2048 302 / 368; 4096 x 4096 1203 / 2175
 //   512 x 2048 200, 249 / 121, 128; 512 x 4608, five of them 353, 362 / 346, 282; 1024 x 4096, four of them 450, 446 / 606, 470;
 //   2048 x 8192 721, 636 / 995, 773
-void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
+void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
 {
     const double workers = std::max(1, c->launch.sm_count / 2);
     // tiles: of the symmetric products of all matrices of this kind
@@ -330,38 +332,54 @@ void choose_shapes(const demo_muon_ctx *c, std::vector<MuonMat> *all)
             }
         return std::max(1.0, n);
     };
-    double best = 0;
+    struct Load {
+        double total = 0, chain = 0;  // us: of all tasks, one after the other; of the longest chain of products
+        double time(double w) const { return std::max(total / w, chain) + 0.3 * std::min(total / w, chain); }
+    };
+    auto load = [&](bool precise, int tile, bool twos) {
+        // us: of a step of K, of a task beside its steps, from a product's last step to the next one's first
+        const double step = precise ? 0.4 : tile == 256 ? 0.28 : 0.2, task = tile == 256 ? 1.5 : 1.0, handover = tile == 256 ? 8.5 : 5.0;
+        Load l;
+        const double square = all_tiles(tile, precise);
+        const MuonMat *last = nullptr;
+        double last_total = 0;
+        for (const MuonMat &m : *all) {
+            if ((m.precise != 0) != precise) continue;
+            if (!last || last->m != m.m || last->n != m.n) {
+                MuonMat probe = m;
+                set(probe, tile, twos, square);
+                double one = 0;
+                last_total = 0;
+                for (const MuonProduct &t : products_of(probe, c->cfg.steps)) {
+                    const double rows = ceil_div(t.m, tile), cols = ceil_div(t.width, tile);
+                    const double tiles = (t.phase < MUON_UPDATE ? rows * (rows + 1) / 2 : rows * cols) * t.splits;
+                    last_total += tiles * (t.steps * step + task);
+                    one += std::ceil(tiles / workers) * (t.steps * step + task) + handover + (t.splits > 1 ? 2 : 0);
+                }
+                l.chain = std::max(l.chain, one);
+                last = &m;
+            }
+            l.total += last_total;
+        }
+        return l;
+    };
+    Load best;
     int best_tile = 0;
     bool best_twos = false;
     for (const int tile : {256, 128})
         for (const bool twos : {true, false}) {
-            // us: of a step of K, of a task beside its steps, from a product's last step to the next one's first
-            const double step = tile == 256 ? 0.28 : 0.2, task = tile == 256 ? 1.5 : 1.0, handover = tile == 256 ? 8.5 : 5.0;
-            double total = 0, chain = 0;
-            const double square = all_tiles(tile, false);
-            const MuonMat *last = nullptr;
-            double last_total = 0;
-            for (MuonMat &m : *all) {
-                if (m.precise) continue;
-                if (!last || last->m != m.m || last->n != m.n) {
-                    MuonMat probe = m;
-                    set(probe, tile, twos, square);
-                    double one = 0;
-                    last_total = 0;
-                    for (const MuonProduct &t : products_of(probe, c->cfg.steps)) {
-                        const double rows = ceil_div(t.m, tile), cols = ceil_div(t.width, tile);
-                        const double tiles = (t.phase < MUON_UPDATE ? rows * (rows + 1) / 2 : rows * cols) * t.splits;
-                        last_total += tiles * (t.steps * step + task);
-                        one += std::ceil(tiles / workers) * (t.steps * step + task) + handover + (t.splits > 1 ? 2 : 0);
-                    }
-                    chain = std::max(chain, one);
-                    last = &m;
-                }
-                total += last_total;
-            }
-            const double time = std::max(total / workers, chain) + 0.3 * std::min(total / workers, chain);
-            if (!best_tile || time < best) best = time, best_tile = tile, best_twos = twos;
+            const Load l = load(false, tile, twos);
+            if (!best_tile || l.time(workers) < best.time(workers)) best = l, best_tile = tile, best_twos = twos;
         }
+    const Load side = load(true, 128, false);
+    if (side.total > 0 && best.total > 0) {
+        // Both kinds at once: as few workers for the small ones as let them end well before the larger ones.  (Those of the larger ones stay until
+        // their last task is done: were they as many as the device holds, the small ones would come after them.)
+        auto both = [&](double w) { return std::max(1.5 * (side.total / w + side.chain), best.time(workers - w)); };
+        c->side_workers = 1;
+        for (int w = 2; w < (int)workers; ++w)
+            if (both(w) < both(c->side_workers)) c->side_workers = w;
+    }
     const double squares[2] = {all_tiles(best_tile, false), all_tiles(best_tile, true)};
     for (MuonMat &m : *all) set(m, best_tile, best_twos, squares[m.precise != 0]);
 }
