@@ -161,105 +161,109 @@ __device__ __forceinline__ void clear_pads(const MuonMat &mat, int i, int j)
             }
 }
 
-// A tile of 64 x 64 elements of X.
-__global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, const MuonTile *tiles, int first_mat, int n_mats, int arrived, int n_arrived)
+// Tiles of 64 x 64 elements of X, `each` one after the other to a CTA: the first one's look-ups, three loads that wait for one another, serve the
+// others, too (67 million elements, 142 us one tile a CTA, 123 four, 134 eight).
+__global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, const MuonTile *tiles, int n_tiles, int each, int first_mat, int n_mats, int arrived, int n_arrived)
 {
     const StreamOrder order(1);
     constexpr int T = MUON_PACK_TILE;
     __shared__ float tile[T][T + 1];
-    const MuonTile t = tiles[blockIdx.x];
-    const MuonMat &mat = a.mats[t.mat];
-    const int transposed = mat.transposed, rows = transposed ? mat.n : mat.m, cols = transposed ? mat.m : mat.n;
-    // tile row i0, column j0 of X; of the tensor, the other way round where X is its transpose
-    const int i0 = t.i * T, j0 = t.j * T;
-    const int r0 = transposed ? j0 : i0, c0 = transposed ? i0 : j0;
     const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;  // four elements of a row, sixteen rows at a time
     constexpr int ROWS = NORM_THREADS / 16;
     order.begin();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.next_task = 0;
     for (int k = blockIdx.x * NORM_THREADS + threadIdx.x; k < n_mats; k += gridDim.x * NORM_THREADS) a.done[first_mat + k] = 0;
     for (int k = blockIdx.x * NORM_THREADS + threadIdx.x; k < n_arrived; k += gridDim.x * NORM_THREADS) a.arrived[arrived + k] = 0;
-    const void *in = a.in[mat.tensor];
-    const float *mom = a.from == MUON_FROM_STEP ? a.mom[mat.tensor] : nullptr;
-    float u[T / ROWS][4];
-    const bool whole = (cols & 3) == 0;
+    for (int n = blockIdx.x * each, end = min(n_tiles, n + each); n < end; ++n) {
+        const MuonTile t = tiles[n];
+        const MuonMat &mat = a.mats[t.mat];
+        const int transposed = mat.transposed, rows = transposed ? mat.n : mat.m, cols = transposed ? mat.m : mat.n;
+        // tile row i0, column j0 of X; of the tensor, the other way round where X is its transpose
+        const int i0 = t.i * T, j0 = t.j * T;
+        const int r0 = transposed ? j0 : i0, c0 = transposed ? i0 : j0;
+        const void *in = a.in[mat.tensor];
+        const float *mom = a.from == MUON_FROM_STEP ? a.mom[mat.tensor] : nullptr;
+        float u[T / ROWS][4];
+        const bool whole = (cols & 3) == 0;
 #pragma unroll
-    for (int k = 0; k < T / ROWS; ++k) {
-        const int r = r0 + y + k * ROWS, c = c0 + x;
-        const long long at = (long long)r * cols + c;
-        float m[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < T / ROWS; ++k) {
+            const int r = r0 + y + k * ROWS, c = c0 + x;
+            const long long at = (long long)r * cols + c;
+            float m[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int l = 0; l < 4; ++l) u[k][l] = 0.f;
-        if (r < rows) {
-            if (whole && c < cols) {
-                if (a.in_bf16) {
-                    const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(in) + at);
-                    u[k][0] = __uint_as_float(v.x << 16);
-                    u[k][1] = __uint_as_float(v.x & 0xffff0000u);
-                    u[k][2] = __uint_as_float(v.y << 16);
-                    u[k][3] = __uint_as_float(v.y & 0xffff0000u);
-                } else {
-                    const float4 v = *reinterpret_cast<const float4 *>(static_cast<const float *>(in) + at);
-                    u[k][0] = v.x, u[k][1] = v.y, u[k][2] = v.z, u[k][3] = v.w;
+            for (int l = 0; l < 4; ++l) u[k][l] = 0.f;
+            if (r < rows) {
+                if (whole && c < cols) {
+                    if (a.in_bf16) {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(in) + at);
+                        u[k][0] = __uint_as_float(v.x << 16);
+                        u[k][1] = __uint_as_float(v.x & 0xffff0000u);
+                        u[k][2] = __uint_as_float(v.y << 16);
+                        u[k][3] = __uint_as_float(v.y & 0xffff0000u);
+                    } else {
+                        const float4 v = *reinterpret_cast<const float4 *>(static_cast<const float *>(in) + at);
+                        u[k][0] = v.x, u[k][1] = v.y, u[k][2] = v.z, u[k][3] = v.w;
+                    }
+                    if (mom) {
+                        const float4 v = *reinterpret_cast<const float4 *>(mom + at);
+                        m[0] = v.x, m[1] = v.y, m[2] = v.z, m[3] = v.w;
+                    }
+                } else if (!whole) {
+#pragma unroll
+                    for (int l = 0; l < 4; ++l)
+                        if (c + l < cols) {
+                            u[k][l] = load_in(in, at + l, a.in_bf16);
+                            if (mom) m[l] = mom[at + l];
+                        }
                 }
                 if (mom) {
-                    const float4 v = *reinterpret_cast<const float4 *>(mom + at);
-                    m[0] = v.x, m[1] = v.y, m[2] = v.z, m[3] = v.w;
+#pragma unroll
+                    for (int l = 0; l < 4; ++l) u[k][l] = a.nesterov ? fmaf(a.mu, m[l], u[k][l]) : m[l];
                 }
-            } else if (!whole) {
-#pragma unroll
-                for (int l = 0; l < 4; ++l)
-                    if (c + l < cols) {
-                        u[k][l] = load_in(in, at + l, a.in_bf16);
-                        if (mom) m[l] = mom[at + l];
-                    }
-            }
-            if (mom) {
-#pragma unroll
-                for (int l = 0; l < 4; ++l) u[k][l] = a.nesterov ? fmaf(a.mu, m[l], u[k][l]) : m[l];
             }
         }
-    }
-    const float2 scale = a.scales[t.mat];
-#pragma unroll
-    for (int k = 0; k < T / ROWS; ++k)
-#pragma unroll
-        for (int l = 0; l < 4; ++l) u[k][l] = u[k][l] * scale.x * scale.y;
-    if (transposed) {
+        const float2 scale = a.scales[t.mat];
 #pragma unroll
         for (int k = 0; k < T / ROWS; ++k)
 #pragma unroll
-            for (int l = 0; l < 4; ++l) tile[x + l][y + k * ROWS] = u[k][l];
-    } else {
+            for (int l = 0; l < 4; ++l) u[k][l] = u[k][l] * scale.x * scale.y;
+        if (transposed) {
 #pragma unroll
-        for (int k = 0; k < T / ROWS; ++k)
+            for (int k = 0; k < T / ROWS; ++k)
 #pragma unroll
-            for (int l = 0; l < 4; ++l) tile[y + k * ROWS][x + l] = u[k][l];
-    }
-    __syncthreads();
+                for (int l = 0; l < 4; ++l) tile[x + l][y + k * ROWS] = u[k][l];
+        } else {
 #pragma unroll
-    for (int k = 0; k < T / ROWS; ++k) {
-        const int i = y + k * ROWS;
-        if (i0 + i < mat.m) {  // (j < ldx, a multiple of the tile's side)
-            const size_t at = (size_t)(i0 + i) * mat.ldx + j0 + x;
-            float w[4];
+            for (int k = 0; k < T / ROWS; ++k)
 #pragma unroll
-            for (int l = 0; l < 4; ++l) w[l] = tile[i][x + l];
-            *reinterpret_cast<uint2 *>(mat.xhi[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
-            if (mat.tile == 128) clear_pads(mat, i0 + i, j0 + x);
-            if (mat.precise) {
+                for (int l = 0; l < 4; ++l) tile[y + k * ROWS][x + l] = u[k][l];
+        }
+        __syncthreads();
 #pragma unroll
-                for (int l = 0; l < 4; ++l) w[l] -= __half2float(__float2half_rn(w[l]));
-                *reinterpret_cast<uint2 *>(mat.xlo[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
+        for (int k = 0; k < T / ROWS; ++k) {
+            const int i = y + k * ROWS;
+            if (i0 + i < mat.m) {  // (j < ldx, a multiple of the tile's side)
+                const size_t at = (size_t)(i0 + i) * mat.ldx + j0 + x;
+                float w[4];
+#pragma unroll
+                for (int l = 0; l < 4; ++l) w[l] = tile[i][x + l];
+                *reinterpret_cast<uint2 *>(mat.xhi[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
+                if (mat.tile == 128) clear_pads(mat, i0 + i, j0 + x);
+                if (mat.precise) {
+#pragma unroll
+                    for (int l = 0; l < 4; ++l) w[l] -= __half2float(__float2half_rn(w[l]));
+                    *reinterpret_cast<uint2 *>(mat.xlo[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
+                }
+            }
+            // block k of the tile's four, a warp for each of its groups of four columns
+            const int lane = threadIdx.x & 31, quad = threadIdx.x >> 5, bi = k >> 1, bj = k & 1;
+            if (i0 + 32 * bi < mat.m) {
+                const float *from = &tile[32 * bi + lane][32 * bj + 4 * quad];
+                float *to = mat.x32 + ((size_t)(i0 / 32 + bi) * (mat.ldx / 32) + j0 / 32 + bj) * 1024 + quad * 128 + lane * 4;
+                *reinterpret_cast<float4 *>(to) = make_float4(from[0], from[1], from[2], from[3]);
             }
         }
-        // block k of the tile's four, a warp for each of its groups of four columns
-        const int lane = threadIdx.x & 31, quad = threadIdx.x >> 5, bi = k >> 1, bj = k & 1;
-        if (i0 + 32 * bi < mat.m) {
-            const float *from = &tile[32 * bi + lane][32 * bj + 4 * quad];
-            float *to = mat.x32 + ((size_t)(i0 / 32 + bi) * (mat.ldx / 32) + j0 / 32 + bj) * 1024 + quad * 128 + lane * 4;
-            *reinterpret_cast<float4 *>(to) = make_float4(from[0], from[1], from[2], from[3]);
-        }
+        __syncthreads();  // (the next tile comes into the same place)
     }
 }
 
@@ -1098,12 +1102,13 @@ cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n
     return demo_launch_kernel(reinterpret_cast<const void *>(muon_norm_kernel), n_pieces, NORM_THREADS, 0, stream, params);
 }
 
-cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, int arrived, int n_arrived, DemoLaunch &,
+cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, int arrived, int n_arrived, DemoLaunch &dev,
                              cudaStream_t stream)
 {
     MuonArgs args = a;
-    void *params[] = {&args, &tiles, &first_mat, &n_mats, &arrived, &n_arrived};
-    return demo_launch_kernel(reinterpret_cast<const void *>(muon_pack_kernel), n_tiles, NORM_THREADS, 0, stream, params);
+    int each = n_tiles >= 32 * dev.sm_count ? 4 : 1;
+    void *params[] = {&args, &tiles, &n_tiles, &each, &first_mat, &n_mats, &arrived, &n_arrived};
+    return demo_launch_kernel(reinterpret_cast<const void *>(muon_pack_kernel), (n_tiles + each - 1) / each, NORM_THREADS, 0, stream, params);
 }
 
 cudaError_t muon_launch_products(int tile, bool precise, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream)
