@@ -126,7 +126,7 @@ cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_til
                              cudaStream_t stream);
 // All products, by pairs of CTAs.  precise: tiles of 128, of hi and lo parts.
 cudaError_t muon_launch_products(int tile, bool precise, const MuonArgs &a, const MuonProduct *products, const MuonTask *tasks, int n_tasks, int workers, DemoLaunch &dev, cudaStream_t stream);
-// Warps of an epilogue; each is a completion of a task in both CTAs.  (Sixteen for tiles of 128, too: 256 x 512 116 us instead of 107; eight of
-// 32 columns for tiles of 256: the 300M-class layers 11.2 ms instead of 10.9.)
+// Warps of an epilogue; each is a completion of a task in both CTAs.  (When they were chosen: sixteen for tiles of 128, too, 256 x 512 116 us
+// instead of 107; eight of 32 columns for tiles of 256, the 300M-class layers 11.2 ms instead of 10.9.)
 constexpr int muon_k_step(int tile) { return 16384 / tile; }
 constexpr int muon_epilogue_warps(int tile) { return tile == 256 ? 16 : 8; }

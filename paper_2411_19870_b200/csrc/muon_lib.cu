@@ -304,9 +304,9 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
 // Tiles of 256 multiply fastest (twice the products for the bytes that a CTA loads), those of 128 pass from one product to the next fastest (5
 // us instead of 8.5).  Which counts for a set is estimated from both: its tasks spread over the workers, and its longest chain of products.
 // Measured, us, tiles of 256 / 128, one after the other and in twos where that is not the same:
-//   512 x 512 166 / 96; 1024 x 1024 207 / 128, four of them 228 / 213; 2048 x 2048 302 / 368; 4096 x 4096 1203 / 2175
-//   512 x 2048 200, 249 / 121, 128; 512 x 4608, five of them 353, 362 / 346, 282; 1024 x 4096, four of them 450, 446 / 606, 470;
-//   2048 x 8192 721, 636 / 995, 773
+//   512 x 512 165 / 92; 1024 x 1024 210 / 115, four of them 230 / 188; 2048 x 2048 302 / 288; 4096 x 4096 1285 / 1780
+//   512 x 2048 205, 232 / 107, 117; 512 x 4608, five of them 338, 329 / 326, 268; 1024 x 4096 265, 289 / 204, 189, four of them 454, 431 / 539, 422;
+//   768 x 8000 318, 311 / 241, 206; 2048 x 8192 682, 594 / 800, 618
 void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
 {
     const double workers = std::max(1, c->launch.sm_count / 2);
@@ -315,11 +315,12 @@ void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
         m.tile = m.precise ? 128 : tile;
         m.twos = twos && !m.precise && c->cfg.steps >= 3 && 2LL * m.n >= 3LL * m.m;
         m.symmetric = m.twos ? 3 : 2;
-        // Sums of up to 8192 elements (32768 where the products are of 11 bits) at a time for their exactness; and long ones in parts of 1024
-        // or more where three quarters of the workers have no tile (300 x 4000: 132 us instead of 143; with tiles for more of them the parts' way
-        // through memory costs what they save: 2048 x 8192 690 instead of 633).
+        // Sums of up to 8192 elements (32768 where the products are of 11 bits) at a time for their exactness; and long ones in three parts of
+        // 1024 or more where half of the workers have no tile (300 x 8000: 146 us instead of 166; 768 x 8000 207 instead of 224; 2048 x 8192 594
+        // instead of 618).  Not more parts
+        // than workers: their way through memory costs more than they save (1024 x 4096 in 144 instead of 72 206 us instead of 189).
         const int steps = ceil_div(m.n, muon_k_step(m.tile)), exact = ceil_div(m.n, m.precise ? 8192 : 32768);
-        const int spread = m.n >= 48 * 64 && 4 * tiles <= workers ? std::min(m.n / 1024, (int)(workers / tiles)) : 1;
+        const int parts = m.n / 1024, spread = parts > 2 && 2 * tiles <= workers ? std::min(parts, (int)(workers / tiles)) : 1;
         m.split_steps = ceil_div(steps, std::max(exact, spread));
         m.splits = ceil_div(steps, m.split_steps);
     };
