@@ -47,7 +47,8 @@ demo_status build(demo_adamw_ctx *c, const int64_t *numels)
         cudaMalloc(&c->d_done, sizeof(unsigned)) != cudaSuccess)
         return DEMO_ERR_ALLOC;
     if (cudaMemcpy(c->d_entries, entries.data(), T * sizeof(AdamwEntry), cudaMemcpyHostToDevice) != cudaSuccess ||
-        cudaMemset(c->d_done, 0, sizeof(unsigned)) != cudaSuccess)
+        cudaMemset(c->d_done, 0, sizeof(unsigned)) != cudaSuccess ||
+        cudaStreamSynchronize(nullptr) != cudaSuccess)  // (the first step may be on a stream that does not wait for this one)
         return DEMO_ERR_CUDA;
     return DEMO_OK;
 }

@@ -548,7 +548,8 @@ demo_status build(demo_muon_ctx *c)
          cudaMemcpy(c->d_products, plan.products.data(), plan.products.size() * sizeof(MuonProduct), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_tasks, plan.tasks.data(), plan.tasks.size() * sizeof(MuonTask), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice) == cudaSuccess &&
-         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess && cudaMemset(c->d_done, 0, (2 * T + 2) * sizeof(unsigned)) == cudaSuccess;
+         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess && cudaMemset(c->d_done, 0, (2 * T + 2) * sizeof(unsigned)) == cudaSuccess &&
+         cudaStreamSynchronize(nullptr) == cudaSuccess;  // (the first call may be on a stream that does not wait for this one)
     return ok ? DEMO_OK : DEMO_ERR_CUDA;
 }
 
