@@ -16,9 +16,7 @@ struct demo_adamw_ctx {
     DemoLaunch launch;
     long long n_pieces = 0, launches = 0;
     AdamwEntry *d_entries = nullptr;
-    void **d_ptrs = nullptr;  // [4][n_tensors]: gradients, both moments, parameters
-    std::vector<void *> ptrs;
-    bool valid = false;
+    PointerTable table;  // gradients, both moments, parameters
     unsigned *d_done = nullptr;
 };
 
@@ -28,7 +26,7 @@ void release(demo_adamw_ctx *c)
 {
     if (!c) return;
     cudaFree(c->d_entries);
-    cudaFree((void *)c->d_ptrs);
+    c->table.release();
     cudaFree(c->d_done);
     delete c;
 }
@@ -42,8 +40,7 @@ demo_status build(demo_adamw_ctx *c, const int64_t *numels)
         entries[t].n = numels[t];
         c->n_pieces += (numels[t] + ADAMW_PIECE - 1) / ADAMW_PIECE;
     }
-    c->ptrs.assign(4 * T, nullptr);
-    if (cudaMalloc(&c->d_entries, T * sizeof(AdamwEntry)) != cudaSuccess || cudaMalloc((void **)&c->d_ptrs, 4 * T * sizeof(void *)) != cudaSuccess ||
+    if (cudaMalloc(&c->d_entries, T * sizeof(AdamwEntry)) != cudaSuccess || c->table.reserve(4 * T) != DEMO_OK ||
         cudaMalloc(&c->d_done, sizeof(unsigned)) != cudaSuccess)
         return DEMO_ERR_ALLOC;
     if (cudaMemcpy(c->d_entries, entries.data(), T * sizeof(AdamwEntry), cudaMemcpyHostToDevice) != cudaSuccess ||
@@ -101,41 +98,28 @@ demo_status demo_adamw_step(demo_adamw_ctx *ctx, const void *const *grads, float
                             int64_t *step, void *cuda_stream)
 {
     if (!ctx || !grads || !exp_avg || !exp_avg_sq || !params || !step || (reinterpret_cast<uintptr_t>(step) & 7u)) return DEMO_ERR_INVALID_ARG;
-    const size_t T = (size_t)ctx->n_tensors, bytes = T * sizeof(void *);
-    const void *lists[4] = {grads, exp_avg, exp_avg_sq, params};
-    bool same = ctx->valid;
-    for (int l = 0; l < 4; ++l) {
-        const void *const *p = static_cast<const void *const *>(lists[l]);
+    const size_t T = (size_t)ctx->n_tensors;
+    const PointerTable::List lists[4] = {{grads, T},
+                                         {reinterpret_cast<const void *const *>(exp_avg), T},
+                                         {reinterpret_cast<const void *const *>(exp_avg_sq), T},
+                                         {reinterpret_cast<const void *const *>(params), T}};
+    for (const PointerTable::List &l : lists)
         for (size_t t = 0; t < T; ++t)
-            if (!p[t] || !aligned16(p[t])) return DEMO_ERR_INVALID_ARG;
-        same = same && std::memcmp(ctx->ptrs.data() + l * T, p, bytes) == 0;
-    }
+            if (!l.pointers[t] || !aligned16(l.pointers[t])) return DEMO_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return DEMO_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (!same) {
-        // (a captured graph would copy whatever the host array holds when it runs)
-        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-        if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess) {
-            cudaGetLastError();
-            return DEMO_ERR_CUDA;
-        }
-        if (capture != cudaStreamCaptureStatusNone) return DEMO_ERR_INVALID_ARG;
-        for (int l = 0; l < 4; ++l) std::memcpy(ctx->ptrs.data() + l * T, lists[l], bytes);
-        ctx->valid = cudaMemcpyAsync((void *)ctx->d_ptrs, ctx->ptrs.data(), 4 * bytes, cudaMemcpyHostToDevice, stream) == cudaSuccess;
-        if (!ctx->valid) {
-            cudaGetLastError();
-            return DEMO_ERR_CUDA;
-        }
-    }
+    const demo_status st = ctx->table.sync({lists[0], lists[1], lists[2], lists[3]}, stream);
+    if (st != DEMO_OK) return st;
+    void **const d_ptrs = ctx->table.dev();
     AdamwArgs a{};
     a.entries = ctx->d_entries;
     a.n_entries = ctx->n_tensors;
     a.n_pieces = ctx->n_pieces;
-    a.g = ctx->d_ptrs;
-    a.m = reinterpret_cast<float *const *>(ctx->d_ptrs + T);
-    a.v = reinterpret_cast<float *const *>(ctx->d_ptrs + 2 * T);
-    a.x = reinterpret_cast<float *const *>(ctx->d_ptrs + 3 * T);
+    a.g = d_ptrs;
+    a.m = reinterpret_cast<float *const *>(d_ptrs + T);
+    a.v = reinterpret_cast<float *const *>(d_ptrs + 2 * T);
+    a.x = reinterpret_cast<float *const *>(d_ptrs + 3 * T);
     a.step = reinterpret_cast<long long *>(step);
     a.done = ctx->d_done;
     a.beta1 = ctx->cfg.beta1;

@@ -59,9 +59,7 @@ struct demo_ctx {
     float **d_x = nullptr;           // [T]
     const DemoRecord **d_p = nullptr;  // [W]
     signed char **d_s = nullptr;       // [T] sign tensors of the parameter-server form
-    float **d_r = nullptr;             // [T] where demo_decode_momentum writes
-    std::vector<float *> h_r;
-    bool r_valid = false;
+    PointerTable momentum_table;       // demo_decode_momentum: [T] where it writes, [W] payloads
     std::vector<signed char *> h_s;
     bool s_valid = false;
     DemoFlatEntry *d_flat = nullptr;   // [T] element ranges for demo_apply_signs
@@ -140,7 +138,7 @@ void release(demo_ctx *c)
     cudaFree((void *)c->d_x);
     cudaFree((void *)c->d_p);
     cudaFree((void *)c->d_s);
-    cudaFree((void *)c->d_r);
+    c->momentum_table.release();
     cudaFree(c->d_flat);
     cudaFree(c->d_tm_g);
     cudaFree(c->d_tm_m);
@@ -715,26 +713,19 @@ static demo_status decode_common(demo_ctx *ctx, const void *const *payloads, int
     }
 
     if (momentum) {
-        // (tables of its own: those of a captured demo_decode_apply stay as they are)
-        const bool same = ctx->r_valid && ctx->p_valid && std::memcmp(ctx->h_r.data(), params, sizeof(float *) * (size_t)T) == 0 &&
-                          std::memcmp(ctx->h_p.data(), payloads, sizeof(void *) * (size_t)W) == 0;
-        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-        if (!same && cudaStreamIsCapturing(stream, &capture) != cudaSuccess) {
-            cudaGetLastError();
-            return DEMO_ERR_CUDA;
-        }
-        if (capture != cudaStreamCaptureStatusNone) return DEMO_ERR_INVALID_ARG;
-        if (!ctx->d_r) {
-            try {
-                ctx->h_r.assign((size_t)T, nullptr);
-            } catch (const std::bad_alloc &) {
-                return DEMO_ERR_ALLOC;
-            }
-            if (cudaMalloc((void **)&ctx->d_r, (size_t)T * sizeof(void *)) != cudaSuccess) {
+        PointerTable &t = ctx->momentum_table;
+        if (!t.reserved()) {
+            cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+            if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess) {
                 cudaGetLastError();
-                return DEMO_ERR_ALLOC;
+                return DEMO_ERR_CUDA;
             }
+            if (capture != cudaStreamCaptureStatusNone) return DEMO_ERR_INVALID_ARG;
+            const demo_status st = t.reserve((size_t)(T + W));
+            if (st != DEMO_OK) return st;
         }
+        const demo_status st = t.sync({{reinterpret_cast<const void *const *>(params), (size_t)T}, {payloads, (size_t)W}}, stream);
+        if (st != DEMO_OK) return st;
         // the kernels add R to what is there
         if (cudaMemsetAsync(momentum, 0, momentum_bytes, stream) != cudaSuccess) {
             cudaGetLastError();
@@ -742,12 +733,11 @@ static demo_status decode_common(demo_ctx *ctx, const void *const *payloads, int
         }
     }
 
-    cudaError_t err = sync_table<const DemoRecord *>(ctx->d_p, ctx->h_p.data(),
-                                                     reinterpret_cast<const DemoRecord *const *>(payloads), W,
-                                                     &ctx->p_valid, stream);
-    if (err == cudaSuccess && momentum)
-        err = sync_table<float *>(ctx->d_r, ctx->h_r.data(), params, T, &ctx->r_valid, stream);
-    else if (err == cudaSuccess && params)
+    cudaError_t err = cudaSuccess;
+    if (!momentum)
+        err = sync_table<const DemoRecord *>(ctx->d_p, ctx->h_p.data(), reinterpret_cast<const DemoRecord *const *>(payloads), W,
+                                             &ctx->p_valid, stream);
+    if (err == cudaSuccess && params && !momentum)
         err = sync_table<float *>(ctx->d_x, ctx->h_x.data(), const_cast<float *const *>(params), T, &ctx->x_valid,
                                   stream);
     if (err == cudaSuccess && signs)
@@ -786,9 +776,9 @@ static demo_status decode_common(demo_ctx *ctx, const void *const *payloads, int
     }
 
     DemoDecodeArgs a;
-    a.payloads = ctx->d_p;
+    a.payloads = momentum ? reinterpret_cast<const DemoRecord *const *>(ctx->momentum_table.dev() + T) : ctx->d_p;
     a.W = W;
-    a.x_ptrs = momentum ? ctx->d_r : ctx->d_x;
+    a.x_ptrs = momentum ? reinterpret_cast<float *const *>(ctx->momentum_table.dev()) : ctx->d_x;
     a.C = ctx->custom_basis ? ctx->d_P : ctx->d_C;
     a.lr = ctx->cfg.lr;
     a.wd = ctx->cfg.weight_decay;

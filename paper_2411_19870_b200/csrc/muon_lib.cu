@@ -29,16 +29,6 @@ struct Group {
     int arrived, n_arrived;  // counters of the parts of its sums
 };
 
-// Pointer arrays of an entry point: device table and mirror, uploaded when they change.
-struct Tables {
-    const void **d_in = nullptr;
-    float **d_mom = nullptr;
-    void **d_out = nullptr;
-    std::vector<const void *> in;
-    std::vector<float *> mom;
-    std::vector<void *> out;
-    bool valid = false;
-};
 enum { FROM_ORTHOGONALIZE = 0, FROM_STEP = 1, FROM_DECODE = 2, ENTRY_POINTS = 3 };
 
 constexpr long long GROUP_ELEMENTS = 128LL << 20;  // workspace: 8 bytes for each, and up to 18 bytes for each of the square matrices beside X
@@ -73,7 +63,7 @@ struct demo_muon_ctx {
     // which the caller's stream waits for (five matrices of 512 rows and one of 147: 302 us, the five alone 293).
     cudaStream_t side_stream = nullptr;
     cudaEvent_t fork = nullptr, join = nullptr;
-    Tables tables[ENTRY_POINTS];
+    PointerTable tables[ENTRY_POINTS];  // inputs, outputs, and momenta where they are the caller's
     float *d_momentum = nullptr;  // reconstructed momenta of demo_muon_decode_apply, from its first call
     size_t momentum_bytes = 0;
     std::vector<float *> momentum_ptrs;
@@ -99,11 +89,7 @@ void release(demo_muon_ctx *c)
     if (c->fork) cudaEventDestroy(c->fork);
     if (c->join) cudaEventDestroy(c->join);
     if (c->side_stream) cudaStreamDestroy(c->side_stream);
-    for (Tables &t : c->tables) {
-        cudaFree((void *)t.d_in);
-        cudaFree((void *)t.d_mom);
-        cudaFree((void *)t.d_out);
-    }
+    for (PointerTable &t : c->tables) t.release();
     delete c;
 }
 
@@ -518,12 +504,7 @@ demo_status build(demo_muon_ctx *c)
               alloc(c, &c->d_scales, T * sizeof(float2)) && alloc(c, &c->d_arrived, (plan.arrived + 1) * sizeof(unsigned)) &&
               alloc(c, &c->d_maps, T * MUON_MAPS * MUON_MAP_BYTES) && alloc(c, &c->d_work, plan.work[0] + plan.work[1]) &&
               alloc(c, &c->d_partials, (size_t)(plan.pieces[0] + plan.pieces[1]) * sizeof(double)) && alloc(c, &c->d_status, sizeof(int));
-    for (Tables &t : c->tables) {
-        ok = ok && alloc(c, (void **)&t.d_in, T * sizeof(void *)) && alloc(c, (void **)&t.d_mom, T * sizeof(void *)) && alloc(c, (void **)&t.d_out, T * sizeof(void *));
-        t.in.assign(T, nullptr);
-        t.mom.assign(T, nullptr);
-        t.out.assign(T, nullptr);
-    }
+    for (int e = 0; e < ENTRY_POINTS; ++e) ok = ok && c->tables[e].reserve((e == FROM_STEP ? 3 : 2) * T) == DEMO_OK;
     if (ok && plan.work[0] && plan.work[1])
         ok = cudaStreamCreateWithFlags(&c->side_stream, cudaStreamNonBlocking) == cudaSuccess && cudaEventCreateWithFlags(&c->fork, cudaEventDisableTiming) == cudaSuccess &&
              cudaEventCreateWithFlags(&c->join, cudaEventDisableTiming) == cudaSuccess;
@@ -553,38 +534,14 @@ demo_status build(demo_muon_ctx *c)
     return ok ? DEMO_OK : DEMO_ERR_CUDA;
 }
 
-// The tables of an entry point for these pointers.  A table that a captured graph would have to copy is refused: the graph would copy
-// whatever the host array holds when it runs.
-demo_status sync_tables(demo_muon_ctx *c, Tables &t, const void *const *in, float *const *mom, void *const *out, cudaStream_t stream)
-{
-    const size_t bytes = (size_t)c->n_tensors * sizeof(void *);
-    if (t.valid && !std::memcmp(t.in.data(), in, bytes) && (!mom || !std::memcmp(t.mom.data(), mom, bytes)) && !std::memcmp(t.out.data(), out, bytes)) return DEMO_OK;
-    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess) {
-        cudaGetLastError();
-        return DEMO_ERR_CUDA;
-    }
-    if (capture != cudaStreamCaptureStatusNone) return DEMO_ERR_INVALID_ARG;
-    t.valid = false;
-    std::memcpy(t.in.data(), in, bytes);
-    if (mom) std::memcpy(t.mom.data(), mom, bytes);
-    std::memcpy(t.out.data(), out, bytes);
-    bool ok = cudaMemcpyAsync(t.d_in, t.in.data(), bytes, cudaMemcpyHostToDevice, stream) == cudaSuccess;
-    ok = ok && (!mom || cudaMemcpyAsync(t.d_mom, t.mom.data(), bytes, cudaMemcpyHostToDevice, stream) == cudaSuccess);
-    ok = ok && cudaMemcpyAsync(t.d_out, t.out.data(), bytes, cudaMemcpyHostToDevice, stream) == cudaSuccess;
-    t.valid = ok;
-    if (!ok) cudaGetLastError();
-    return ok ? DEMO_OK : DEMO_ERR_CUDA;
-}
-
-demo_status run(demo_muon_ctx *c, MuonArgs a, const Tables &t, cudaStream_t stream)
+demo_status run(demo_muon_ctx *c, MuonArgs a, const PointerTable &t, cudaStream_t stream)
 {
     const demo_muon_config &g = c->cfg;
     a.mats = c->d_mats;
     a.maps = c->d_maps;
-    a.in = t.d_in;
-    a.mom = t.d_mom;
-    a.out = t.d_out;
+    a.in = const_cast<const void *const *>(t.dev());
+    a.out = t.dev() + c->n_tensors;
+    a.mom = a.from == MUON_FROM_STEP ? reinterpret_cast<float *const *>(t.dev() + 2 * (size_t)c->n_tensors) : nullptr;
     a.done = c->d_done;
     a.ready = c->d_done + c->n_tensors;
     a.scales = c->d_scales;
@@ -694,8 +651,9 @@ demo_status demo_orthogonalize(demo_muon_ctx *ctx, const void *const *in, int32_
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return DEMO_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    Tables &t = ctx->tables[FROM_ORTHOGONALIZE];
-    const demo_status st = sync_tables(ctx, t, in, nullptr, out, stream);
+    PointerTable &t = ctx->tables[FROM_ORTHOGONALIZE];
+    const size_t T = (size_t)ctx->n_tensors;
+    const demo_status st = t.sync({{in, T}, {out, T}}, stream);
     if (st != DEMO_OK) return st;
     MuonArgs a{};
     a.from = MUON_FROM_INPUT;
@@ -714,8 +672,9 @@ demo_status demo_muon_step(demo_muon_ctx *ctx, const void *const *grads, float *
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return DEMO_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    Tables &t = ctx->tables[FROM_STEP];
-    const demo_status st = sync_tables(ctx, t, grads, momentum, reinterpret_cast<void *const *>(params), stream);
+    PointerTable &t = ctx->tables[FROM_STEP];
+    const size_t T = (size_t)ctx->n_tensors;
+    const demo_status st = t.sync({{grads, T}, {reinterpret_cast<const void *const *>(params), T}, {reinterpret_cast<const void *const *>(momentum), T}}, stream);
     if (st != DEMO_OK) return st;
     MuonArgs a{};
     a.from = MUON_FROM_STEP;
@@ -765,8 +724,8 @@ demo_status demo_muon_decode_apply(demo_muon_ctx *ctx, demo_ctx *demo, const voi
             table[i] = place[i] < 0 ? params[i] : ctx->momentum_ptrs[(size_t)place[i]];
             if (place[i] >= 0) out[(size_t)place[i]] = params[i];
         }
-        Tables &t = ctx->tables[FROM_DECODE];
-        demo_status done = sync_tables(ctx, t, reinterpret_cast<const void *const *>(ctx->momentum_ptrs.data()), nullptr, out.data(), stream);
+        PointerTable &t = ctx->tables[FROM_DECODE];
+        demo_status done = t.sync({{reinterpret_cast<const void *const *>(ctx->momentum_ptrs.data()), out.size()}, {out.data(), out.size()}}, stream);
         if (done != DEMO_OK) return done;
         done = demo_decode_momentum(demo, payloads, n_payloads, table.data(), ctx->d_momentum, ctx->momentum_bytes, stream);
         if (done != DEMO_OK) return done;
@@ -786,7 +745,13 @@ demo_status demo_muon_set_lr(demo_muon_ctx *ctx, float lr)
     return DEMO_OK;
 }
 
-size_t demo_muon_workspace_bytes(const demo_muon_ctx *ctx) { return ctx ? ctx->bytes : 0; }
+size_t demo_muon_workspace_bytes(const demo_muon_ctx *ctx)
+{
+    size_t tables = 0;
+    if (ctx)
+        for (const PointerTable &t : ctx->tables) tables += t.bytes();
+    return ctx ? ctx->bytes + tables : 0;
+}
 
 int64_t demo_muon_launch_count(const demo_muon_ctx *ctx) { return ctx ? ctx->launches : 0; }
 

@@ -140,3 +140,86 @@ def test_types_and_places_are_checked_on_the_device():
     tr.orthogonalize([u], [o])
     torch.cuda.synchronize()
     assert tr.device_status() == 0 and tr.launch_count == 3 and adam.launch_count == 0
+
+
+def replayed_between_calls_with_others(call, make):
+    """call(a) captured; then called with b, and captured with b, too; the graphs still work on their own tensors, call by call."""
+    a, b, c, want_a, want_b = (make() for _ in range(5))
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.stream(st):
+        call(a)
+        st.synchronize()
+        with torch.cuda.graph(graphs[0], stream=st):
+            call(a)
+        call(c)
+        graphs[0].replay()
+        call(b)
+        st.synchronize()
+        with torch.cuda.graph(graphs[1], stream=st):
+            call(b)
+        call(c)
+        graphs[1].replay()
+        graphs[0].replay()
+    st.synchronize()
+    for _ in range(3):
+        call(want_a)
+    for _ in range(2):
+        call(want_b)
+    call(make())
+    torch.cuda.synchronize()
+    for got, want in ((a, want_a), (b, want_b), (c, want_b)):
+        assert all(torch.equal(u, v) for x, y in zip(got, want) for u, v in zip(x, y))
+
+
+def test_a_captured_step_keeps_its_tensors():
+    shapes = [(64, 96), (300, 400)]
+    tr = muon(shapes, grad_dtype=demo.DEMO_F32)
+    make = lambda: [[rand(s, k * 10 + i) for i, s in enumerate(shapes)] for k in range(3)]  # noqa: E731
+    replayed_between_calls_with_others(lambda s: tr.step(*s), make)
+    assert tr.device_status() == 0
+
+
+def test_a_captured_orthogonalisation_keeps_its_tensors():
+    shapes = [(64, 96), (300, 400)]
+    tr = muon(shapes)
+    make = lambda: [[rand(s, i) for i, s in enumerate(shapes)]]  # noqa: E731
+    before = tr.workspace_bytes
+    replayed_between_calls_with_others(lambda s: tr.orthogonalize(s[0], s[0]), make)  # (in place)
+    assert tr.device_status() == 0 and before < tr.workspace_bytes < before + 4096
+
+
+def test_a_captured_adamw_step_keeps_its_tensors():
+    shapes = [(64, 96), (301,)]
+    tr = demo.AdamwTransform(shapes, lr=1e-2, weight_decay=0.1, grad_dtype=demo.DEMO_F32)
+    counts = []
+
+    def make():
+        s = [[rand(sh, k * 10 + i).abs() for i, sh in enumerate(shapes)] for k in range(4)]
+        counts.append(torch.zeros(1, dtype=torch.int64, device="cuda"))
+        return s + [[counts[-1]]]
+
+    replayed_between_calls_with_others(lambda s: tr.step(s[0], s[1], s[2], s[3], s[4][0]), make)
+    assert [int(c) for c in counts] == [3, 2, 2, 3, 2, 1]
+
+
+def test_a_captured_decode_keeps_its_tensors():
+    shapes = [(128, 192), (64,), (320, 384)]
+    tr = demo.DemoTransform(shapes, chunk=64, topk=32, beta=0.9, lr=1e-2, weight_decay=0.1, num_workers=2)
+    tr_mu = muon([shapes[0], shapes[2]])
+
+    def payload(seed):
+        p = torch.empty(tr.payload_bytes, dtype=torch.uint8, device="cuda")
+        tr.compress(0, [rand(s, seed + i).bfloat16() for i, s in enumerate(shapes)], [torch.zeros(s, device="cuda") for s in shapes], p)
+        return p
+
+    def make():
+        return [[payload(1), payload(5)], [rand(s, i) for i, s in enumerate(shapes)]]
+
+    def call(s):
+        tr_mu.decode_apply(tr, s[0], s[1])
+        tr.decode_apply([s[0][1], s[0][0]], [t.clone() for t in s[1]]) if not torch.cuda.is_current_stream_capturing() else None
+
+    replayed_between_calls_with_others(call, make)
+    assert tr_mu.device_status() == 0 and tr.device_status() == 0
