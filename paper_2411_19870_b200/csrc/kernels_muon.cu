@@ -88,6 +88,8 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_norm_kernel(MuonArgs a, int
         sum += (double)g * (double)g;
     };
     const int len = (int)(n - at < a.piece ? n - at : a.piece);
+    if (at == 0 && !mat.precise)
+        for (int i = threadIdx.x; i < mat.m; i += NORM_THREADS) mat.rest[0][i] = mat.rest[1][i] = 0;
 #pragma unroll 4
     for (int i = threadIdx.x * 4; i + 3 < len; i += NORM_THREADS * 4) {
         float g[4];
@@ -137,6 +139,10 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_norm_kernel(MuonArgs a, int
         a.scales[e] = make_float2(scale1, (float)(scale / (double)scale1));
     }
 }
+
+// x^2 - h^2, and a sum of them as MuonMat's `rest` holds it
+__device__ __forceinline__ float add_rest(float sum, float x, float h) { return fmaf(x - h, x + h, sum); }
+__device__ __forceinline__ int rest_units(float sum, float inv_S) { return __float2int_rn(sum * inv_S * inv_S * MUON_REST); }
 
 __device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
 __device__ __forceinline__ uint32_t pack2(float x, float y)
@@ -242,6 +248,7 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
 #pragma unroll
         for (int k = 0; k < T / ROWS; ++k) {
             const int i = y + k * ROWS;
+            float rest = 0.f;
             if (i0 + i < mat.m) {  // (j < ldx, a multiple of the tile's side)
                 const size_t at = (size_t)(i0 + i) * mat.ldx + j0 + x;
                 float w[4];
@@ -253,7 +260,15 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
 #pragma unroll
                     for (int l = 0; l < 4; ++l) w[l] -= __half2float(__float2half_rn(w[l]));
                     *reinterpret_cast<uint2 *>(mat.xlo[0] + at) = make_uint2(pack2(w[0], w[1]), pack2(w[2], w[3]));
+                } else {
+#pragma unroll
+                    for (int l = 0; l < 4; ++l) rest = add_rest(rest, w[l], __half2float(__float2half_rn(w[l])));
                 }
+            }
+            if (!mat.precise) {
+#pragma unroll
+                for (int d = 8; d; d >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, d);
+                if (x == 0 && i0 + i < mat.m) atomicAdd(mat.rest[0] + i0 + i, rest_units(rest, mat.inv_S));
             }
             // block k of the tile's four, a warp for each of its groups of four columns
             const int lane = threadIdx.x & 31, quad = threadIdx.x >> 5, bi = k >> 1, bj = k & 1;
@@ -523,15 +538,18 @@ __device__ __forceinline__ float take_own(const BlockAt &b, float (&v)[16])
 __device__ __forceinline__ bool on_diagonal(const BlockAt &b) { return (b.r0 ^ b.j0) < 32; }  // (both below 2^31, multiples of 32 and 16)
 __device__ __forceinline__ bool has_own(const BlockAt &b) { return (unsigned)(b.r0 + b.lane - b.j0) < 16u; }
 
-// E = A off the diagonal, d on it.  v: the products.
+// E = A off the diagonal, d on it.  v: the products; rest: what the row's own lacks.
 template <int TILE, bool PRECISE>
-__device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &b, float (&v)[16])
+__device__ __forceinline__ void block_gram(const MuonProduct &t, const BlockAt &b, float (&v)[16], float rest)
 {
 #pragma unroll
     for (int k = 0; k < 16; ++k) v[k] *= t.scale;
     if (on_diagonal(b)) {
         const float own = take_own(b, v);
-        if (has_own(b)) __stcg(t.diag + b.r0 + b.lane, own * MUON_EF_INV);
+        if (has_own(b)) {
+            __stcg(t.diag + b.r0 + b.lane, fmaf(own, MUON_EF_INV, rest));
+            if (!PRECISE && b.r0 + b.lane < t.m) __stcg(t.rest + b.r0 + b.lane, 0);
+        }
     }
     stage_halves<TILE, PRECISE>(b, v);
     store_block(t.dst + b.fp32, v);
@@ -589,12 +607,24 @@ __device__ __forceinline__ void block_mul(const MuonProduct &t, const BlockAt &b
 
 // X <- B X
 template <int TILE, bool PRECISE>
-__device__ __forceinline__ void block_update(const MuonProduct &t, const BlockAt &b, const float4 (&x)[4], float di)
+__device__ __forceinline__ void block_update(const MuonProduct &t, const BlockAt &b, const float4 (&x)[4], float di, float &rest)
 {
     float v[16];
     tmem_ld16(b.tmem, v);
 #pragma unroll
     for (int k = 0; k < 16; ++k) v[k] = fmaf(di, part(x, k), v[k] * MUON_EF_INV);
+    if (!PRECISE) {
+        if (t.width - b.j0 < 16) {  // (what is outside the matrix is no part of it)
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (k >= t.width - b.j0) v[k] = 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 16; k += 2) {
+            const float2 h = unpack2(pack2(v[k], v[k + 1]));
+            rest = add_rest(add_rest(rest, v[k], h.x), v[k + 1], h.y);
+        }
+    }
     stage_halves<TILE, PRECISE>(b, v);
     store_block(t.dst + b.fp32, v);
 }
@@ -969,6 +999,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 load_block(t.src + place(0), next);
                 row = __ldcg(t.vec + r0 + lane);
             }
+            if (!PRECISE && t.phase == MUON_GRAM && ti == tj && r0 + lane < t.m) row = (float)__ldcg(t.rest + r0 + lane) * MUON_REST_INV;
             if (t.phase == MUON_FINAL && a.to == MUON_TO_PARAMS) {  // the parameters' rows on their way to L2
                 const int rows = t.transposed ? t.width : t.m, cols = t.transposed ? t.m : t.width;
                 for (int b = 0; b < 16 * blocks; b += 32) {
@@ -1029,15 +1060,17 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     } else {
                         add_parts(parts + b.number * 512, t.splits, part_stride, v);
                     }
-                    block_gram<TILE, PRECISE>(t, b, v);
+                    block_gram<TILE, PRECISE>(t, b, v, row);
                 });
             else if (t.phase == MUON_POLY)
                 each_block([&](const BlockAt &b) { block_poly<TILE, PRECISE>(a, t, b, x, row); });
             else if (t.phase == MUON_MUL)
                 each_block([&](const BlockAt &b) { block_mul<TILE, PRECISE>(t, b, x, row); });
-            else if (t.phase == MUON_UPDATE)
-                each_block([&](const BlockAt &b) { block_update<TILE, PRECISE>(t, b, x, row); });
-            else
+            else if (t.phase == MUON_UPDATE) {
+                float rest = 0.f;
+                each_block([&](const BlockAt &b) { block_update<TILE, PRECISE>(t, b, x, row, rest); });
+                if (!PRECISE && blocks > 0 && r0 + lane < t.m) atomicAdd(t.rest + r0 + lane, rest_units(rest, t.scale));
+            } else
                 each_block([&](const BlockAt &b) { block_final(a, t, b, x, row, b.number + 1 < blocks); });
             if (blocks > 0 && t.phase != MUON_FINAL) {
                 // (pad rows and columns: the copy leaves out what lies outside the matrix)

@@ -40,6 +40,7 @@ struct MuonMat {
     uint16_t *xhi[2], *xlo[2];
     uint16_t *ehi[MUON_SYMMETRIC], *elo[MUON_SYMMETRIC];
     float *x32, *e32[MUON_SYMMETRIC], *diag[MUON_SYMMETRIC];
+    int *rest[2];      // of both X, by row, in MUON_REST: what the squares of the fp16 values leave out (not `precise` ones)
     // GRAM's sum over K is cut into `splits` parts of `split_steps` steps, which lie in `parts` until the last of them adds them up
     int splits, split_steps;
     int arrived;       // index of its first counter: one for each tile, CTA and warp of the epilogue
@@ -56,6 +57,11 @@ constexpr int MUON_MAP_BYTES = 128;
 // Off the diagonal, symmetric matrices lie in the workspace 256 times as large: entries of 1/m and less, and their lo parts, stay in fp16's normal range (of rank one,
 // 96 rows: error 1.6e-4 without).  Entries of up to 255 remain possible: singular values up to about 3 within the iterations.
 constexpr float MUON_EF_SCALE = 256.f, MUON_EF_INV = 1.f / 256.f;
+
+// The diagonal of X X^T takes the squares of X's fp32 values: where one entry of a row outweighs the others, the rounding of its fp16 value, which
+// elsewhere averages out, is that of the result (heavy-tailed 830 x 3320: entries off by up to 1.6e-3 of it, instead of 3e-4).  What is missing is
+// summed up in whole multiples of 2^-38, in any order to the same bits: 2^-11 of the squares, below 2^31 multiples for singular values up to 16.
+constexpr float MUON_REST = 274877906944.f, MUON_REST_INV = 1.f / 274877906944.f;
 
 constexpr int MUON_PACK_TILE = 64;   // side of the tiles in which X is laid out
 
@@ -86,7 +92,10 @@ struct alignas(16) MuonProduct {  // what the tasks of one product of one matrix
     const float *src2;       // MUL: the right factor; GRAM: the parts
     float *dst;              // fp32 result, NULL: not needed
     const float *vec;        // POLY, MUL: the left factor's diagonal; UPDATE, FINAL: the polynomial's
-    const float *vec2;       // MUL: the right factor's diagonal
+    union {
+        const float *vec2;   // MUL: the right factor's diagonal
+        int *rest;           // GRAM: of the X that is read, zero afterwards; UPDATE: of the one that is written
+    };
     float *diag;             // the result's diagonal
     float scale, step_scale; // GRAM: of A off the diagonal; FINAL: of O, of the update
     int last_steps;          // the last part's

@@ -127,6 +127,7 @@ size_t place(MuonMat &m, size_t at)
     }
     m.x32 = reinterpret_cast<float *>(take(rows * (size_t)m.ldx * 4));
     m.parts = reinterpret_cast<float *>(m.splits > 1 ? reinterpret_cast<size_t>(take((size_t)m.splits * (size_t)tiles_above(m) * (size_t)(m.tile * m.tile) * 4)) : 0);
+    for (int p = 0; p < 2; ++p) m.rest[p] = m.precise ? nullptr : reinterpret_cast<int *>(take((size_t)m.m * 4));
     for (int k = 0; k < m.symmetric; ++k) {
         m.ehi[k] = take(e);
         m.elo[k] = m.precise ? take(e) : m.ehi[k];
@@ -141,6 +142,7 @@ void rebase(MuonMat &m, char *base)
     for (int p = 0; p < 2; ++p) {
         move(m.xhi[p]);
         move(m.xlo[p]);
+        if (!m.precise) move(m.rest[p]);
     }
     move(m.x32);
     move(m.parts);
@@ -202,6 +204,7 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
         MuonProduct &t = add(MUON_GRAM);
         x_maps(t.left, t.left_lo, now);
         x_maps(t.right, t.right_lo, now);
+        t.rest = m.rest[now];
         result(t, to, true);
     };
     auto multiply = [&](int phase, int p, int q, int to, bool fp32) {
@@ -221,6 +224,7 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
         t.src = t.dst = m.x32;
         t.vec = m.diag[by];
         now ^= 1;
+        t.rest = last ? nullptr : m.rest[now];
         x_maps(t.out, t.out_lo, now);
     };
     for (int k = 0; k < steps;) {
