@@ -6,18 +6,20 @@
 //   GRAM    A = X X^T                        symmetric: the tiles on and above the diagonal
 //   POLY    B = a + b A + c A^2, from A^2     symmetric, too
 //   UPDATE  X <- B X
-// Wide matrices do two iterations in one: the second's A is A B^2, a polynomial of the first's, and X <- (B' B) X is multiplied once,
+// Wide matrices do the first two iterations in one: the second's A is A B^2, a polynomial of the first's, and X <- (B' B) X is multiplied once,
 //   GRAM, POLY, MUL T = A B, MUL A' = T B, POLY B', MUL Q = B' B, UPDATE
 // which for n = 4 m takes 17 m^3 instead of 26 and reads and writes X once.
 // Operands are fp16 (11 bits, accumulated in fp32), and what would lose accuracy in them is kept out of them:
 //   * the linear term, on which small singular values live alone (they grow by a = 3.4 an iteration, rounding noise with them), and all
 //     other sums outside the products are formed from fp32 copies;
 //   * the diagonals of symmetric matrices, of order one in the last iterations, where a X and (b A + c A^2) X nearly cancel, never pass
-//     through fp16: with P = D + E, Q = D' + E', P Q = D D' + D E' + E D' + E E', and only E E' is a product on the tensor cores.
-// Relative error of the result against 64 bits, 1024 x 4096: Gaussian 2e-4, of rank one 8e-4, of rank 32 2e-3 (plain bf16 operands, one
-// iteration after the other: 1.3e-2, 1.2 and 0.2; fp16: 1.7e-3, 0.15 and 0.03).  It grows as matrices shrink, so those of up to 256 rows take
-// the lo parts of the products' operands, too.  All five iterations in one would take 29 m^3 for n = 4 m, where two at a time take 47, but
-// noise outside a low rank then grows to 0.15: B' B of two iterations is at most a^2 = 12, of five 480, and is rounded to 11 bits.
+//     through fp16: with P = D + E, Q = D' + E', P Q = D D' + D E' + E D' + E E', and only E E' is a product on the tensor cores; and that
+//     of X X^T is the one of X's fp32 values (muon.h, MUON_REST).
+// Relative error of the result against 64 bits, 1024 x 4096: Gaussian 3e-4, of rank 1, 32 and 128 9e-4, 6e-4 and 9e-4; 400 x 1200 5e-4 and 1.4e-3,
+// 1.2e-3, 1.7e-3 (plain bf16 operands, 1024 x 4096: Gaussian 1.3e-2, of rank 1 and 32 1.2 and 0.2; fp16: 1.7e-3, 0.15 and 0.03).  It grows as
+// matrices shrink, so those of up to 384 rows take the lo parts of the products' operands, too.  More iterations in one would multiply less (all
+// five 29 m^3 for n = 4 m instead of 56), but their B' B is rounded to 11 bits after the last one that could take noise away: [1, 2, 2] has up to
+// five times the error where the rank is low, [5] an error of 0.15.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -29,7 +29,7 @@ struct MuonMat {
     int transposed;    // 1: X is the tensor's transpose
     int precise;       // 1: products take the lo parts, too
     int tile;          // side of the products' tiles
-    int twos;          // 1: two iterations in one
+    int twos;          // 1: the first two iterations in one
     int tensor;        // position in the caller's pointer arrays
     int piece_begin;   // its first piece of the norm in the group, and how many
     int n_pieces;
@@ -60,8 +60,9 @@ constexpr float MUON_EF_SCALE = 256.f, MUON_EF_INV = 1.f / 256.f;
 
 // The diagonal of X X^T takes the squares of X's fp32 values: where one entry of a row outweighs the others, the rounding of its fp16 value, which
 // elsewhere averages out, is that of the result (heavy-tailed 830 x 3320: entries off by up to 1.6e-3 of it, instead of 3e-4).  What is missing is
-// summed up in whole multiples of 2^-38, in any order to the same bits: 2^-11 of the squares, below 2^31 multiples for singular values up to 16.
-constexpr float MUON_REST = 274877906944.f, MUON_REST_INV = 1.f / 274877906944.f;
+// summed up in whole multiples of 2^-36, in any order to the same bits: 2^-10 of the squares at most, below 2^31 multiples for singular values up
+// to 5, beyond what MUON_EF_SCALE admits.
+constexpr float MUON_REST = 68719476736.f, MUON_REST_INV = 1.f / 68719476736.f;
 
 constexpr int MUON_PACK_TILE = 64;   // side of the tiles in which X is laid out
 

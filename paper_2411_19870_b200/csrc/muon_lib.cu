@@ -32,7 +32,10 @@ struct Group {
 enum { FROM_ORTHOGONALIZE = 0, FROM_STEP = 1, FROM_DECODE = 2, ENTRY_POINTS = 3 };
 
 constexpr long long GROUP_ELEMENTS = 128LL << 20;  // workspace: 8 bytes for each, and up to 18 bytes for each of the square matrices beside X
-constexpr int PRECISE_SIDE = 256;                 // up to here the products take the lo parts, too (kernels_muon.cu)
+// Up to here the products take the lo parts, too (kernels_muon.cu): what 11 bits lose grows as matrices shrink, and small products are quick.
+// (384: an error of 1.6e-3 where the rank is low, as 384 x 768 decoded from few records, is 1e-5, for 113 us instead of 93, fourteen of 384 x 384 135
+// instead of 113, sixty of 384 x 1536 1360 instead of 800.  512: five of 512 x 4608 would take twice as long.)
+constexpr int PRECISE_SIDE = 384;
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
 
@@ -228,8 +231,10 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
         x_maps(t.out, t.out_lo, now);
     };
     for (int k = 0; k < steps;) {
-        // the first alone: [1, 2, 2] has a third of the error of [2, 2, 1] where the rank is low
-        const bool two = m.twos && k > 0 && k + 2 <= steps;
+        // The first two only: what the products of two iterations round adds noise where the rank is low, and from the first ones the later
+        // iterations take it away again.  (1024 x 2048 of rank 1, 5, 32, 128: [2, 1, 1, 1] 9e-4, 4e-4, 6e-4, 9e-4, which is what one after the other gives;
+        // [1, 2, 2], which would multiply 16 % less at n = 4 m, 6e-4, 3e-3, 2e-3, 4e-3.)
+        const bool two = m.twos && k == 0;
         gram(0);
         multiply(MUON_POLY, 0, 0, 1, two);
         if (two) {
@@ -290,25 +295,25 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
 }
 
 // Sets the tile and the way of the iterations of every matrix.
-// Two iterations in one take 3 r + 5 products of m^3 multiplications, one after the other 6 r + 2, r = n / m, but are one product longer.
+// The first two iterations in one take 3 r + 5 products of m^3 multiplications, one after the other 6 r + 2, r = n / m, but are one product longer.
 // Tiles of 256 multiply fastest (twice the products for the bytes that a CTA loads), those of 128 pass from one product to the next fastest (5
 // us instead of 8.5).  Which counts for a set is estimated from both: its tasks spread over the workers, and its longest chain of products.
-// Measured, us, tiles of 256 / 128, one after the other and in twos where that is not the same:
-//   512 x 512 165 / 92; 1024 x 1024 210 / 115, four of them 230 / 188; 2048 x 2048 302 / 288; 4096 x 4096 1285 / 1780
-//   512 x 2048 205, 232 / 107, 117; 512 x 4608, five of them 338, 329 / 326, 268; 1024 x 4096 265, 289 / 204, 189, four of them 454, 431 / 539, 422;
-//   768 x 8000 318, 311 / 241, 206; 2048 x 8192 682, 594 / 800, 618
+// Measured, us, tiles of 256 / 128, one after the other and with the first two in one where that is not the same:
+//   512 x 512 170 / 94; 1024 x 1024 213 / 116, four of them 238 / 193; 2048 x 2048 314 / 299; 4096 x 4096 1380 / 1810
+//   512 x 2048 206, 220 / 109, 114; 512 x 4608, five of them 349, 346 / 337, 310; 1024 x 4096 273, 286 / 212, 204, four of them 473, 460 / 552, 498;
+//   768 x 8000 334, 330 / 250, 233; 2048 x 8192 697, 653 / 834, 737
 void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
 {
     const double workers = std::max(1, c->launch.sm_count / 2);
     // tiles: of the symmetric products of all matrices of this kind
     auto set = [&](MuonMat &m, int tile, bool twos, double tiles) {
         m.tile = m.precise ? 128 : tile;
-        m.twos = twos && !m.precise && c->cfg.steps >= 3 && 2LL * m.n >= 3LL * m.m;
+        m.twos = twos && !m.precise && c->cfg.steps >= 2 && 2LL * m.n >= 3LL * m.m;
         m.symmetric = m.twos ? 3 : 2;
         // Sums of up to 8192 elements (32768 where the products are of 11 bits) at a time for their exactness; and long ones in three parts of
-        // 1024 or more where half of the workers have no tile (300 x 8000: 146 us instead of 166; 768 x 8000 207 instead of 224; 2048 x 8192 594
-        // instead of 618).  Not more parts
-        // than workers: their way through memory costs more than they save (1024 x 4096 in 144 instead of 72 206 us instead of 189).
+        // 1024 or more where half of the workers have no tile.  Not more parts than workers: their way through memory costs more than they save.
+        // (Both with every second pair of iterations in one: 768 x 8000 207 us instead of 224, 2048 x 8192 594 instead of 618; 1024 x 4096 in 144
+        // parts instead of 72 206 instead of 189.)
         const int steps = ceil_div(m.n, muon_k_step(m.tile)), exact = ceil_div(m.n, m.precise ? 8192 : 32768);
         const int parts = m.n / 1024, spread = parts > 2 && 2 * tiles <= workers ? std::min(parts, (int)(workers / tiles)) : 1;
         m.split_steps = ceil_div(steps, std::max(exact, spread));

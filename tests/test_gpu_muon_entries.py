@@ -21,7 +21,9 @@ def orthogonalised(shape, count, u):
 
 # tiles of 128 (one, two at a time), transposed, sums in parts, tiles of 256 (many), hi and lo parts; sizes within a tile's first row of blocks too
 @pytest.mark.parametrize("shape,count", [((300, 301), 1), ((300, 1200), 1), ((1201, 300), 1), ((300, 4003), 1), ((300, 420), 160), ((270, 1333), 160),
-                                         ((420, 300), 160), ((257, 257), 1), ((100, 130), 1)])
+                                         ((420, 300), 160), ((257, 257), 1), ((100, 130), 1),
+                                         ((400, 401), 1), ((400, 1600), 1), ((1601, 400), 1), ((400, 4003), 1), ((400, 520), 160), ((390, 1533), 160),
+                                         ((520, 400), 160)])
 def test_one_entry_a_row(shape, count):
     gen = torch.Generator("cuda").manual_seed(1)
     m, n = min(shape), max(shape)

@@ -20,7 +20,7 @@ def rand(shape, seed, scale=1.0):
 
 # tiles of 128 with hi and lo parts, of 128, of 256 (many of them), both kinds at once, sums in parts; odd sizes, so that there are pads
 @pytest.mark.parametrize("shapes", [[(65, 127)], [(129, 1000), (33, 70)], [(257, 331)], [(300, 700)], [(270, 1333)] * 160, [(147, 99), (513, 700)],
-                                    [(301, 4001)], [(700, 8200)], [(3, 9001)]], ids=range(9))
+                                    [(301, 4001)], [(700, 8200)], [(3, 9001)], [(401, 555)], [(401, 1333)], [(390, 1333)] * 160, [(401, 4001)]], ids=range(13))
 def test_nothing_of_a_bad_matrix_stays(shapes):
     tr, fresh = muon(shapes), muon(shapes)
     ins = [rand(s, i) for i, s in enumerate(shapes)]
