@@ -63,7 +63,7 @@ struct demo_muon_ctx {
     int side_workers = 0;   // workers of the precise matrices where there are others, too
     int *d_status = nullptr;
     // Where there are matrices of both kinds, the precise ones go through the iterations beside the others, on a stream of the context's own,
-    // which the caller's stream waits for (five matrices of 512 rows and one of 147: 302 us, the five alone 293).
+    // which the caller's stream waits for (five matrices of 512 rows and one of 147: 344 us, the five alone 335, the one 107).
     cudaStream_t side_stream = nullptr;
     cudaEvent_t fork = nullptr, join = nullptr;
     PointerTable tables[ENTRY_POINTS];  // inputs, outputs, and momenta where they are the caller's
@@ -253,8 +253,9 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
 
 // The products of the matrices mats[0 .. n), `first` the index of the first.  Matrices go through the iterations in cohorts, product by product,
 // every product matrix by matrix: with two rounds of the workers' tasks in a cohort's symmetric products, a matrix's next product starts when its last
-// is done.  (24 layers of a 1024-wide decoder: rounds 2 or 3 11.4 ms, 1.5 12.0, 1 13.4, 0.5 19.4; and 11.6 in the order in which workers of a
-// model of the device would start the tasks, with as few matrices under way as that takes.)  Returns how many workers the tasks keep busy.
+// is done.  (48 of 2048 x 2048: 9.6 ms with two rounds, 10.3 with one, 9.5 to 9.8 with three to twelve; 60 of 1024 x 1024 2.36, 2.54 and
+// 2.2 to 2.35.  Less than one takes up to twice as long, and an order in which workers of a model of the device would start the tasks, with as few
+// matrices under way as that takes, as long as two rounds.)  Returns how many workers the tasks keep busy.
 int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int side, Plan *plan)
 {
     const int device = std::max(1, c->launch.sm_count / 2);
