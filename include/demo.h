@@ -357,8 +357,10 @@ demo_status demo_set_momentum_domain(demo_ctx *ctx, int32_t domain);
  * 8 bytes an element more; demo_muon_workspace_bytes tells.
  *
  * Accuracy: products of fp16 operands accumulated in fp32; everything else, the linear term and the diagonals among it, in fp32.  Against
- * 64 bits O has a relative error (Frobenius norm) of up to 1e-3, 2e-3 where U has a low rank; 1e-5, 2e-4 where the smaller
- * side is at most 384, whose products take 22 bits.  Entries that outweigh their row and column are as exact as the others.  Sums over a longer side n add n 2^-27, at most 1e-4.
+ * 64 bits O has a relative error (Frobenius norm) of up to 1e-3, 2e-3 where U has not full rank; where the smaller side is at most 384, whose
+ * products take 22 bits, of up to 2e-5 and, over a longer side n, n 2^-26 (6e-5 at most), 4e-4 where U has not full rank.  All this takes for granted that roundings
+ * average out.  Those of equal entries do not: a matrix of equal entries, rows or columns, or of many that differ in sign alone, is off by up to
+ * 3e-2 (4e-4).  Entries that outweigh their row and column are as exact as the others.
  * Coefficients under which singular values grow beyond about 3 in the iterations leave the range of fp16: unspecified values.  NaN or Inf in a
  * matrix make its own result unspecified and no other's; a matrix of zeros gives zeros.  Results do not depend on the order of
  * execution: the same call on the same data gives the same bits.
