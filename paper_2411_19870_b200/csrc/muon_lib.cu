@@ -313,11 +313,12 @@ void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
         m.symmetric = m.twos ? 3 : 2;
         // Sums of up to 2048 elements (8192 where the products are of 11 bits) at a time for their exactness: what the tensor core cuts off all goes
         // one way (160 of 64 x 8192, Gaussian / all entries equal: error 4.9e-5 / 5.2e-4 in 3.59 ms at 8192 at a time, 1.1e-5 / 6.4e-5 in 3.66 ms at
-        // 2048; 50304 x 384 692, 722, 808 us at 8192, 4096, 2048; 60 of 400 x 32768, all equal: 1.5e-2 in 16.3 ms at 32768, 3e-3 in 14.2 ms at 8192).  And long ones in three parts of
+        // 2048; 50304 x 384 692, 722, 808 us at 8192, 4096, 2048; 60 of 400 x 32768, all equal: 1.5e-2 in 16.3 ms at 32768, 3e-3 in 14.2 ms at 8192).
+        // (From m = 8192 on parts of m, at most 32768: the other products' sums are as long, and a part takes 2 m^2 bytes.)  And long ones in three parts of
         // 1024 or more where half of the workers have no tile.  Not more parts than workers: their way through memory costs more than they save.
         // (Both with every second pair of iterations in one: 768 x 8000 207 us instead of 224, 2048 x 8192 594 instead of 618; 1024 x 4096 in 144
         // parts instead of 72 206 instead of 189.)
-        const int steps = ceil_div(m.n, muon_k_step(m.tile)), exact = ceil_div(m.n, m.precise ? 2048 : 8192);
+        const int steps = ceil_div(m.n, muon_k_step(m.tile)), exact = ceil_div(m.n, m.precise ? 2048 : std::min(32768, std::max(8192, m.m)));
         const int parts = m.n / 1024, spread = parts > 2 && 2 * tiles <= workers ? std::min(parts, (int)(workers / tiles)) : 1;
         m.split_steps = ceil_div(steps, std::max(exact, spread));
         m.splits = ceil_div(steps, m.split_steps);
