@@ -427,7 +427,11 @@ demo_status demo_muon_decode_apply(demo_muon_ctx *ctx, demo_ctx *demo, const voi
 demo_status demo_muon_set_lr(demo_muon_ctx *ctx, float lr);
 /* Bytes of device memory that the context holds, tables and workspace.  0 if ctx is NULL. */
 size_t demo_muon_workspace_bytes(const demo_muon_ctx *ctx);
-/* As demo_launch_count, demo_device_status (DEMO_OK or DEMO_ERR_TIMEOUT) and demo_free. */
+/* Self-test of the products' give-up path, as demo_selftest_bounded_wait: the tasks of one product, started while the product that they need
+ * never comes.  They wait for limit_cycles SM clock cycles (1 .. 2e9) and give up; demo_muon_device_status then says DEMO_ERR_TIMEOUT, once.  Calls
+ * that follow are not affected.  Errors: INVALID_ARG, CUDA. */
+demo_status demo_muon_selftest_bounded_wait(demo_muon_ctx *ctx, int64_t limit_cycles, void *cuda_stream);
+/* As demo_launch_count, demo_device_status (DEMO_OK or DEMO_ERR_TIMEOUT: unspecified results of a call since the last time) and demo_free. */
 int64_t demo_muon_launch_count(const demo_muon_ctx *ctx);
 demo_status demo_muon_device_status(demo_muon_ctx *ctx, void *cuda_stream);
 void demo_muon_free(demo_muon_ctx *ctx);

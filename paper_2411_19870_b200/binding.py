@@ -34,7 +34,7 @@ EXPORTS = [
     "demo_set_basis_gaussian", "demo_get_basis", "demo_selftest_bounded_wait", "demo_set_path", "demo_set_momentum_domain", "demo_launch_count", "demo_device_status",
     "demo_status_string", "demo_free",
     "demo_muon_init", "demo_orthogonalize", "demo_muon_step", "demo_muon_decode_apply", "demo_muon_set_lr", "demo_muon_workspace_bytes",
-    "demo_muon_launch_count", "demo_muon_device_status", "demo_muon_free",
+    "demo_muon_selftest_bounded_wait", "demo_muon_launch_count", "demo_muon_device_status", "demo_muon_free",
     "demo_adamw_init", "demo_adamw_step", "demo_adamw_set_lr", "demo_adamw_launch_count", "demo_adamw_free",
 ]
 
@@ -154,6 +154,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.demo_muon_set_lr.restype = i32
     lib.demo_muon_workspace_bytes.argtypes = [vp]
     lib.demo_muon_workspace_bytes.restype = ctypes.c_size_t
+    lib.demo_muon_selftest_bounded_wait.argtypes = [vp, i64, vp]
+    lib.demo_muon_selftest_bounded_wait.restype = i32
     lib.demo_muon_launch_count.argtypes = [vp]
     lib.demo_muon_launch_count.restype = i64
     lib.demo_muon_device_status.argtypes = [vp, vp]
@@ -605,6 +607,11 @@ class MuonTransform:
 
     def device_status(self, stream=None) -> int:
         return int(self.lib.demo_muon_device_status(self._ctx, DemoTransform._stream_on(stream, self.device)))
+
+    def selftest_bounded_wait(self, limit_cycles: int, stream=None) -> None:
+        st = self.lib.demo_muon_selftest_bounded_wait(self._ctx, int(limit_cycles), DemoTransform._stream_on(stream, self.device))
+        if st != 0:
+            raise DemoError(st, "demo_muon_selftest_bounded_wait")
 
     def close(self) -> None:
         if getattr(self, "_ctx", None) is not None and self._ctx.value:

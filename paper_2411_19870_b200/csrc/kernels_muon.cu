@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(NORM_THREADS) muon_pack_kernel(MuonArgs a, con
     const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;  // four elements of a row, sixteen rows at a time
     constexpr int ROWS = NORM_THREADS / 16;
     order.begin();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.next_task = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.next_task = *a.gave_up = 0;
     for (int k = blockIdx.x * NORM_THREADS + threadIdx.x; k < n_mats; k += gridDim.x * NORM_THREADS) a.done[first_mat + k] = 0;
     for (int k = blockIdx.x * NORM_THREADS + threadIdx.x; k < n_arrived; k += gridDim.x * NORM_THREADS) a.arrived[arrived + k] = 0;
     for (int n = blockIdx.x * each, end = min(n_tiles, n + each); n < end; ++n) {
@@ -372,9 +372,7 @@ __device__ __forceinline__ void arrive_release_cluster(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-constexpr long long TASK_WAIT_CYCLES = 20000000000LL;  // ~10 s: what is waited for may be other workers' tasks, long ones for large matrices
-
-__device__ __forceinline__ bool wait_local(uint32_t bar, unsigned parity) { return mbar_wait_bounded(bar, parity, TASK_WAIT_CYCLES); }
+__device__ __forceinline__ bool wait_local(uint32_t bar, unsigned parity, const MuonArgs &a) { return mbar_wait_bounded(bar, parity, a.wait_cycles); }
 // One lane of a warp that runs converged.  The loading and the MMA warp loop with all their lanes and leave only the instructions themselves to
 // one: operands formed in divergent code cost each MMA and each copy 100 to 200 cycles on their way to uniform registers (a step of a 256 tile
 // 581 cycles instead of 512, which is what the products take; 256 x 512 159 us instead of 136).
@@ -394,7 +392,7 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, unsigned parity)
     return ok != 0;
 }
 // as wait_local, seeing what another CTA of the cluster did before its arrival
-__device__ __forceinline__ bool wait_cluster(uint32_t bar, unsigned parity)
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, unsigned parity, const MuonArgs &a)
 {
     const long long t0 = clock64();
     for (;;) {
@@ -405,7 +403,7 @@ __device__ __forceinline__ bool wait_cluster(uint32_t bar, unsigned parity)
             : "r"(bar), "r"(parity)
             : "memory");
         if (ok) return true;
-        if (clock64() - t0 > TASK_WAIT_CYCLES) return false;
+        if (clock64() - t0 > a.wait_cycles) return false;
     }
 }
 
@@ -696,14 +694,14 @@ __device__ __forceinline__ unsigned load_acquire(const unsigned *p)
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-// Until `need` completions of a matrix are there.  False when that takes too long or another CTA has given up.
-__device__ __forceinline__ bool wait_task(const unsigned *done, unsigned need, const int *status)
+// Until `need` completions of a matrix are there.  False when that takes too long or another CTA of this launch has given up.
+__device__ __forceinline__ bool wait_task(const unsigned *done, unsigned need, const MuonArgs &a)
 {
     if (load_acquire(done) >= need) return true;
     const long long t0 = clock64();
     for (unsigned n = 0; load_acquire(done) < need; ++n) {
         __nanosleep(20);
-        if ((n & 1023) == 1023 && (clock64() - t0 > TASK_WAIT_CYCLES || *static_cast<const volatile int *>(status) != 0)) return false;
+        if ((n & 1023) == 1023 && (clock64() - t0 > a.wait_cycles || *static_cast<const volatile unsigned *>(a.gave_up) != 0)) return false;
     }
     return true;
 }
@@ -787,12 +785,12 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 if (rank == 0) {
                     t = drawn < (unsigned)n_tasks ? (int)drawn : -1;
                     // the second CTA looks the task up, too, while this one waits for what the task needs
-                    ok = wait_cluster(q_empty + 8 * slot, turn ^ 1);
+                    ok = wait_cluster(q_empty + 8 * slot, turn ^ 1, a);
                     if (!ok) break;
                     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(drawn_ring + slot), 1)), "r"(t) : "memory");
                     arrive_release_cluster(map_to_rank(q_full + 8 * slot, 1));
                 } else {
-                    ok = wait_cluster(q_full + 8 * slot, turn);
+                    ok = wait_cluster(q_full + 8 * slot, turn, a);
                     if (!ok) break;
                     t = *static_cast<volatile int *>(drawn_ring + slot);
                     arrive_cluster(map_to_rank(q_empty + 8 * slot, 0));
@@ -822,15 +820,15 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     }
                 }
                 if (rank == 0) {
-                    ok = t < 0 || wait_task(a.done + p.mat, p.need, a.status);
+                    ok = t < 0 || wait_task(a.done + p.mat, p.need, a);
                     if (!ok) break;
                     arrive_release_cluster(map_to_rank(go_full + 8 * slot, 1));
                 } else {
-                    ok = wait_cluster(go_full + 8 * slot, turn);
+                    ok = wait_cluster(go_full + 8 * slot, turn, a);
                     if (!ok) break;
                 }
                 fence_proxy_async_global();  // what other tasks wrote is read by this CTA's copies
-                ok = wait_local(r_empty + 8 * slot, turn ^ 1);
+                ok = wait_local(r_empty + 8 * slot, turn ^ 1, a);
                 if (!ok) break;
                 {
                     uint4 *to = reinterpret_cast<uint4 *>(ring + slot);
@@ -854,7 +852,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     }
                 // The next task is drawn when this one's loads are nearly through: earlier, it would only be kept from other workers.
                 if (rank == 0) {
-                    ok = wait_local(near_end, near_turn);
+                    ok = wait_local(near_end, near_turn, a);
                     if (!ok) break;
                     near_turn ^= 1;
                     drawn = atomicAdd(a.next_task, 1u);
@@ -868,7 +866,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
         int stage = 0;
         unsigned phase = 0, used = 0;
         for (;;) {
-            ok = all_of(wait_local(r_full + 8 * slot, turn));
+            ok = all_of(wait_local(r_full + 8 * slot, turn, a));
             if (!ok) break;
             const RingEntry &e = ring[slot];
             const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
@@ -887,7 +885,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
             for (int k = 0; ok && k < steps; ++k)
                 for (int part = 0; part < parts; ++part) {  // hi, lo
                     if (left_steps-- == near_steps && one && left_side) arrive(near_end);
-                    ok = all_of(wait_local(empty + 8 * stage, phase ^ 1));
+                    ok = all_of(wait_local(empty + 8 * stage, phase ^ 1, a));
                     if (!ok) break;
                     if (one) {
                         if (rank == 0) mbar_expect_tx(full + 8 * stage, 2 * OPERAND);
@@ -902,7 +900,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
         for (int s = 0; s < STAGES && used; ++s) {
             if (used >= (unsigned)STAGES || s < stage) {
                 const unsigned last = s < stage ? phase : phase ^ 1;
-                if (!wait_local(empty + 8 * s, last)) ok = false;
+                if (!wait_local(empty + 8 * s, last, a)) ok = false;
             }
         }
     } else if (warp == MMA) {
@@ -911,7 +909,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
             int stage = 0, n_done = 0;
             unsigned phase = 0;
             for (;; ++n_done) {
-                ok = all_of(wait_local(r_full + 8 * slot, turn));
+                ok = all_of(wait_local(r_full + 8 * slot, turn, a));
                 if (!ok) break;
                 const RingEntry &e = ring[slot];
                 const int end = uniform(e.end), kind = uniform(e.p.phase), steps = uniform(e.steps), parts = PRECISE ? 2 : 1, ti = uniform(e.i), tj = uniform(e.j);
@@ -921,7 +919,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 next_slot();
                 if (end) break;
                 const int acc = n_done & 1;
-                ok = all_of(wait_cluster(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1));
+                ok = all_of(wait_cluster(t_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1, a));
                 if (!ok) break;
                 tc_after();
                 const uint32_t d = tmem + acc * 256;
@@ -940,14 +938,14 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     const uint64_t a_at = operand_desc(0, a_mn ? 8192 : 16, 1024), b_at = operand_desc(0, b_mn ? 8192 : 16, 1024);
                     const uint32_t at = (base + stage * STAGE) >> 4;  // (below 2^14)
                     const uint64_t da = a_at + at, db = b_at + at + (OPERAND >> 4);
-                    ok = all_of(wait_local(full + 8 * stage, phase));
+                    ok = all_of(wait_local(full + 8 * stage, phase, a));
                     if (!ok) break;
                     tc_after();
                     const int hi = stage;
                     if (one) multiply(da, db, idesc, a_mn, b_mn, k ? 1u : 0u);
                     if (++stage == STAGES) stage = 0, phase ^= 1;
                     if (parts > 1) {  // the next stage holds the lo parts
-                        ok = all_of(wait_local(full + 8 * stage, phase));
+                        ok = all_of(wait_local(full + 8 * stage, phase, a));
                         if (!ok) break;
                         tc_after();
                         const uint32_t at_lo = (base + stage * STAGE) >> 4;
@@ -992,7 +990,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
         };
         for (int n_done = 0;; ++n_done) {
             if (!__all_sync(0xffffffffu, mbar_test(r_full + 8 * slot, turn))) tell();
-            ok = wait_local(r_full + 8 * slot, turn);
+            ok = wait_local(r_full + 8 * slot, turn, a);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const MuonProduct &t = ring[slot].p;  // (the slot is free again when the task is done)
@@ -1020,7 +1018,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 }
             }
             tell();
-            ok = wait_local(t_full + 8 * acc, (n_done >> 1) & 1);
+            ok = wait_local(t_full + 8 * acc, (n_done >> 1) & 1, a);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_after();
@@ -1103,7 +1101,10 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
         }
         tell();
     }
-    if (!ok) atomicExch(a.status, DEMO_DEV_TIMEOUT);
+    if (!ok) {
+        atomicExch(a.gave_up, 1u);
+        atomicExch(a.status, DEMO_DEV_TIMEOUT);
+    }
     __syncwarp();
     tc_before();
     __syncthreads();

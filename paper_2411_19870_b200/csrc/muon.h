@@ -118,6 +118,7 @@ struct MuonArgs {
     float2 *scales;        // device: of each matrix, S / (||u|| + eps) in two factors
     unsigned *done;        // device: completions of each matrix's tasks
     unsigned *next_task;   // device
+    unsigned *gave_up;     // device: not 0 once a wait of this launch has run out
     unsigned *arrived;     // device: parts of a sum that are there
     int piece;             // elements of a piece of the norm
     int from, to;
@@ -125,13 +126,14 @@ struct MuonArgs {
     int nesterov;
     float mu, eps, lr, wd;
     float a, b, c;
-    int *status;
+    long long wait_cycles; // limit of each wait of the products
+    int *status;           // DEMO_DEV_TIMEOUT once a wait of any launch has run out, until the host has asked
 };
 
 // Momentum update and the pieces' sums of squares; pieces [0, n_pieces) of the matrices [first, first + n).
 cudaError_t muon_launch_norm(const MuonArgs &a, int first_mat, int n_mats, int n_pieces, DemoLaunch &dev, cudaStream_t stream);
 // X = S u / (||u|| + eps), as hi + lo; clears the counters of the matrices [first_mat, first_mat + n_mats), n_arrived of their parts' from
-// `arrived` on, and the next task.
+// `arrived` on, the next task and the word that tells that a CTA has given up.
 cudaError_t muon_launch_pack(const MuonArgs &a, const MuonTile *tiles, int n_tiles, int first_mat, int n_mats, int arrived, int n_arrived, DemoLaunch &dev,
                              cudaStream_t stream);
 // All products, by pairs of CTAs.  precise: tiles of 128, of hi and lo parts.

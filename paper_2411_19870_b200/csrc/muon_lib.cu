@@ -26,6 +26,7 @@ struct Group {
     int n_pack;
     long long tasks;
     int n_tasks, workers;
+    int waiting, n_waiting;  // those of its first matrix's second product, for the self-test
     int arrived, n_arrived;  // counters of the parts of its sums
 };
 
@@ -36,6 +37,7 @@ constexpr long long GROUP_ELEMENTS = 128LL << 20;  // workspace: 8 bytes for eac
 // (384: an error of 1.6e-3 where the rank is low, as 384 x 768 decoded from few records, is 1e-5, for 113 us instead of 93, fourteen of 384 x 384 135
 // instead of 113, sixty of 384 x 1536 1360 instead of 800.  512: five of 512 x 4608 would take twice as long.)
 constexpr int PRECISE_SIDE = 384;
+constexpr long long WAIT_CYCLES = 20000000000LL;  // ~10 s: what is waited for may be other workers' tasks, long ones for large matrices
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
 
@@ -53,7 +55,7 @@ struct demo_muon_ctx {
     MuonTile *d_tiles = nullptr;
     MuonProduct *d_products = nullptr;
     MuonTask *d_tasks = nullptr;
-    unsigned *d_done = nullptr;  // [n_tensors] completions; [n_tensors] pieces ready; the next task of each kind
+    unsigned *d_done = nullptr;  // [n_tensors] completions; [n_tensors] pieces ready; the next task of each kind; whether it has given up
     float2 *d_scales = nullptr;
     unsigned *d_arrived = nullptr;
     char *d_maps = nullptr;
@@ -468,6 +470,9 @@ demo_status make_tasks(demo_muon_ctx *c, Plan *plan)
         g.tasks = (long long)plan->tasks.size();
         g.workers = add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.tile, plan);
         g.n_tasks = (int)((long long)plan->tasks.size() - g.tasks);
+        const auto waits = [&](long long k) { const MuonProduct &p = plan->products[(size_t)plan->tasks[(size_t)(g.tasks + k)].product]; return p.mat == g.first_mat && p.phase == MUON_POLY; };
+        while (!waits(g.waiting)) ++g.waiting;  // (every matrix has that product)
+        while (g.waiting + g.n_waiting < g.n_tasks && waits(g.waiting + g.n_waiting)) ++g.n_waiting;
         if (plan->tasks.size() > (size_t)(1LL << 30)) return DEMO_ERR_UNSUPPORTED;
     }
     return DEMO_OK;
@@ -513,7 +518,7 @@ demo_status build(demo_muon_ctx *c)
     }
     const size_t T = (size_t)c->n_tensors;
     bool ok = alloc(c, &c->d_mats, T * sizeof(MuonMat)) && alloc(c, &c->d_tiles, plan.tiles.size() * sizeof(MuonTile)) &&
-              alloc(c, &c->d_done, (2 * T + 2) * sizeof(unsigned)) &&
+              alloc(c, &c->d_done, (2 * T + 4) * sizeof(unsigned)) &&
               alloc(c, &c->d_scales, T * sizeof(float2)) && alloc(c, &c->d_arrived, (plan.arrived + 1) * sizeof(unsigned)) &&
               alloc(c, &c->d_maps, T * MUON_MAPS * MUON_MAP_BYTES) && alloc(c, &c->d_work, plan.work[0] + plan.work[1]) &&
               alloc(c, &c->d_partials, (size_t)(plan.pieces[0] + plan.pieces[1]) * sizeof(double)) && alloc(c, &c->d_status, sizeof(int));
@@ -542,23 +547,31 @@ demo_status build(demo_muon_ctx *c)
          cudaMemcpy(c->d_products, plan.products.data(), plan.products.size() * sizeof(MuonProduct), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_tasks, plan.tasks.data(), plan.tasks.size() * sizeof(MuonTask), cudaMemcpyHostToDevice) == cudaSuccess &&
          cudaMemcpy(c->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice) == cudaSuccess &&
-         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess && cudaMemset(c->d_done, 0, (2 * T + 2) * sizeof(unsigned)) == cudaSuccess &&
+         cudaMemset(c->d_status, 0, sizeof(int)) == cudaSuccess && cudaMemset(c->d_done, 0, (2 * T + 4) * sizeof(unsigned)) == cudaSuccess &&
          cudaStreamSynchronize(nullptr) == cudaSuccess;  // (the first call may be on a stream that does not wait for this one)
     return ok ? DEMO_OK : DEMO_ERR_CUDA;
+}
+
+// What the kernels of every call take.
+void fill_common(const demo_muon_ctx *c, MuonArgs *a)
+{
+    a->mats = c->d_mats;
+    a->maps = c->d_maps;
+    a->done = c->d_done;
+    a->ready = c->d_done + c->n_tensors;
+    a->scales = c->d_scales;
+    a->arrived = c->d_arrived;
+    a->wait_cycles = WAIT_CYCLES;
+    a->status = c->d_status;
 }
 
 demo_status run(demo_muon_ctx *c, MuonArgs a, const PointerTable &t, cudaStream_t stream)
 {
     const demo_muon_config &g = c->cfg;
-    a.mats = c->d_mats;
-    a.maps = c->d_maps;
+    fill_common(c, &a);
     a.in = const_cast<const void *const *>(t.dev());
     a.out = t.dev() + c->n_tensors;
     a.mom = a.from == MUON_FROM_STEP ? reinterpret_cast<float *const *>(t.dev() + 2 * (size_t)c->n_tensors) : nullptr;
-    a.done = c->d_done;
-    a.ready = c->d_done + c->n_tensors;
-    a.scales = c->d_scales;
-    a.arrived = c->d_arrived;
     a.nesterov = g.nesterov;
     a.mu = g.momentum;
     a.eps = g.eps;
@@ -567,7 +580,6 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const PointerTable &t, cudaStream_
     a.a = g.coefficients[0];
     a.b = g.coefficients[1];
     a.c = g.coefficients[2];
-    a.status = c->d_status;
     cudaError_t err = cudaSuccess;
     const bool both = c->side_stream != nullptr;
     if (both) {
@@ -581,6 +593,7 @@ demo_status run(demo_muon_ctx *c, MuonArgs a, const PointerTable &t, cudaStream_
             a.partials = c->d_partials + (kind ? c->side_partials : 0);
             a.piece = grp.piece;
             a.next_task = c->d_done + 2 * c->n_tensors + kind;
+            a.gave_up = a.next_task + 2;
             if (err == cudaSuccess) err = muon_launch_norm(a, grp.first_mat, grp.n_mats, grp.n_pieces, c->launch, on);
             if (err == cudaSuccess) err = muon_launch_pack(a, c->d_tiles + grp.pack_tiles, grp.n_pack, grp.first_mat, grp.n_mats, grp.arrived, grp.n_arrived, c->launch, on);
             if (err == cudaSuccess) err = muon_launch_products(grp.tile, grp.precise, a, c->d_products, c->d_tasks + grp.tasks, grp.n_tasks, grp.workers, c->launch, on);
@@ -781,6 +794,28 @@ demo_status demo_muon_device_status(demo_muon_ctx *ctx, void *cuda_stream)
         return DEMO_ERR_CUDA;
     }
     return word == 0 ? DEMO_OK : word == DEMO_DEV_TIMEOUT ? DEMO_ERR_TIMEOUT : DEMO_ERR_CUDA;
+}
+
+demo_status demo_muon_selftest_bounded_wait(demo_muon_ctx *ctx, int64_t limit_cycles, void *cuda_stream)
+{
+    if (!ctx || limit_cycles < 1 || limit_cycles > 2000000000LL) return DEMO_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return DEMO_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const Group &g = ctx->groups.front();
+    MuonArgs a{};
+    fill_common(ctx, &a);
+    a.wait_cycles = limit_cycles;
+    a.next_task = ctx->d_done + 2 * ctx->n_tensors;
+    a.gave_up = a.next_task + 2;
+    // no product is done, no task drawn
+    if (cudaMemsetAsync(ctx->d_done + g.first_mat, 0, sizeof(unsigned), stream) != cudaSuccess || cudaMemsetAsync(a.next_task, 0, 4 * sizeof(unsigned), stream) != cudaSuccess ||
+        muon_launch_products(g.tile, g.precise, a, ctx->d_products, ctx->d_tasks + g.tasks + g.waiting, g.n_waiting, g.workers, ctx->launch, stream) != cudaSuccess) {
+        cudaGetLastError();
+        return DEMO_ERR_CUDA;
+    }
+    ctx->launches += 1;
+    return DEMO_OK;
 }
 
 void demo_muon_free(demo_muon_ctx *ctx)
