@@ -793,7 +793,6 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     ok = wait_cluster(q_full + 8 * slot, turn, a);
                     if (!ok) break;
                     t = *static_cast<volatile int *>(drawn_ring + slot);
-                    arrive_cluster(map_to_rank(q_empty + 8 * slot, 0));
                 }
                 MuonTask tk{0, 0, 0, 0};
                 if (t >= 0) tk = tasks[t];
@@ -826,6 +825,9 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                 } else {
                     ok = wait_cluster(go_full + 8 * slot, turn, a);
                     if (!ok) break;
+                    // The slot is free behind this wait only: where tasks have one step, the first CTA gets as far as the slot's next task before any of
+                    // this one's data is needed, and a barrier that is completed twice looks as if it had never been.
+                    arrive_cluster(map_to_rank(q_empty + 8 * slot, 0));
                 }
                 fence_proxy_async_global();  // what other tasks wrote is read by this CTA's copies
                 ok = wait_local(r_empty + 8 * slot, turn ^ 1, a);
