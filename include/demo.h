@@ -352,9 +352,9 @@ demo_status demo_set_momentum_domain(demo_ctx *ctx, int32_t domain);
  * update: the matrix with its singular values moved towards one by Newton-Schulz iterations,
  *     X = U / (||U||_F + eps);   steps times:  A = X X^T,  X <- a X + (b A + c A^2) X;   O(U) = X
  * (for a matrix with more rows than columns of its transpose).  A demo_muon_ctx belongs to a list of matrices, of any sizes from 1 x 1,
- * and owns the workspace of the iterations: up to 26 bytes an element, extents rounded up to multiples of 64, of as many matrices as make
- * 128 million elements (or of the largest one), which go through the iterations together, and for long sums, cut into parts, up to 20 MB or
- * 8 bytes an element more; demo_muon_workspace_bytes tells.
+ * and owns the workspace of the iterations.  Matrices whose smaller side is at most 384 and all others have one each, of up to 26 bytes an element, extents
+ * rounded up to multiples of 64, and for long sums, cut into parts, up to 20 MB or 8 bytes an element more; no larger than 3.5 GB or what the largest
+ * matrix takes: sets that would need more go through it in groups of up to 128 million elements.  demo_muon_workspace_bytes tells.
  *
  * Accuracy: products of fp16 operands accumulated in fp32; everything else, the linear term and the diagonals among it, in fp32.  Against
  * 64 bits O has a relative error (Frobenius norm) of up to 1e-3, 2e-3 where U has not full rank; where the smaller side is at most 384, whose

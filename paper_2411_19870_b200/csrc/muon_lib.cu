@@ -33,6 +33,7 @@ struct Group {
 enum { FROM_ORTHOGONALIZE = 0, FROM_STEP = 1, FROM_DECODE = 2, ENTRY_POINTS = 3 };
 
 constexpr long long GROUP_ELEMENTS = 128LL << 20;  // workspace: 8 bytes for each, and up to 18 bytes for each of the square matrices beside X
+constexpr size_t GROUP_BYTES = 26 * (size_t)GROUP_ELEMENTS;  // of their workspace: thin matrices take more than 26 bytes an element, up to 145 where there is one row
 // Up to here the products take the lo parts, too (kernels_muon.cu): what 11 bits lose grows as matrices shrink, and small products are quick.
 // (384: an error of 1.6e-3 where the rank is low, as 384 x 768 decoded from few records, is 1e-5, for 113 us instead of 93, fourteen of 384 x 384 135
 // instead of 113, sixty of 384 x 1536 1360 instead of 800.  512: five of 512 x 4608 would take twice as long.)
@@ -431,12 +432,13 @@ demo_status make_plan(demo_muon_ctx *c, Plan *plan)
         for (; end < all.size() && (all[end].precise != 0) == g.precise; ++end) {
             MuonMat &m = all[end];
             const long long n = (long long)m.m * m.n;
-            if (end > at && elements + n > GROUP_ELEMENTS) break;
+            const size_t place_end = place(m, work);
+            if (end > at && (elements + n > GROUP_ELEMENTS || place_end > GROUP_BYTES)) break;
             elements += n;
+            work = place_end;
             m.piece_begin = (int)pieces;
             m.n_pieces = (int)((n + g.piece - 1) / g.piece);
             pieces += m.n_pieces;
-            work = place(m, work);
             m.maps = (int)end * MUON_MAPS;
             m.arrived = (int)(plan->arrived + counters);
             if (m.splits > 1) counters += (size_t)tiles_above(m) * (size_t)(2 * muon_epilogue_warps(m.tile));
