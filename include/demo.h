@@ -367,7 +367,8 @@ demo_status demo_set_momentum_domain(demo_ctx *ctx, int32_t domain);
  *
  * Device buffers are contiguous, 16-byte aligned and, unless stated, not aliased.  Calls on one context, captured graphs among them, are
  * issued in stream order as for demo_ctx: they share its workspace.  Pointer arrays are copied to device tables, of each entry point its
- * own, when they differ from that entry point's last call; a captured graph keeps those it was captured with.  A call that would have to
+ * own, when they differ from that entry point's last call; a captured graph keeps those it was captured with, and gives their table back when it
+ * and what was instantiated from it are destroyed.  A call that would have to
  * copy them on a stream that is being captured returns INVALID_ARG with nothing enqueued (call it once before).  After
  * demo_muon_set_lr a captured graph keeps the rate it was captured with.
  */
