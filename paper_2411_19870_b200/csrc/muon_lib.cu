@@ -26,6 +26,7 @@ struct Group {
     int n_pack;
     long long tasks;
     int n_tasks, workers;
+    int at_once;             // tasks that can be in work at the same time
     int waiting, n_waiting;  // those of its first matrix's second product, for the self-test
     int arrived, n_arrived;  // counters of the parts of its sums
 };
@@ -254,15 +255,21 @@ std::vector<MuonProduct> products_of(const MuonMat &m, int steps)
     return list;
 }
 
+// How many workers one kind of matrices has.
+int workers_for(const demo_muon_ctx *c, bool precise)
+{
+    const int device = std::max(1, c->launch.sm_count / 2);
+    return std::max(1, c->side_workers == 0 ? device : precise ? c->side_workers : device - c->side_workers);
+}
+
 // The products of the matrices mats[0 .. n), `first` the index of the first.  Matrices go through the iterations in cohorts, product by product,
 // every product matrix by matrix: with two rounds of the workers' tasks in a cohort's symmetric products, a matrix's next product starts when its last
 // is done.  (48 of 2048 x 2048: 9.6 ms with two rounds, 10.3 with one, 9.5 to 9.8 with three to twelve; 60 of 1024 x 1024 2.36, 2.54 and
 // 2.2 to 2.35.  Less than one takes up to twice as long, and an order in which workers of a model of the device would start the tasks, with as few
-// matrices under way as that takes, as long as two rounds.)  Returns how many workers the tasks keep busy.
+// matrices under way as that takes, as long as two rounds.)  Returns how many tasks there are at once.
 int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int side, Plan *plan)
 {
-    const int device = std::max(1, c->launch.sm_count / 2);
-    const int workers = std::max(1, c->side_workers == 0 ? device : mats[0].precise ? c->side_workers : device - c->side_workers);
+    const int workers = workers_for(c, mats[0].precise);
     auto symmetric = [&](const MuonMat &m) { const long long k = ceil_div(m.m, side); return k * (k + 1) / 2; };
     long long total = 0;
     for (int e = 0; e < n; ++e) total += symmetric(mats[e]);
@@ -295,7 +302,7 @@ int add_tasks(const demo_muon_ctx *c, const MuonMat *mats, int first, int n, int
             most = std::max(most, plan->tasks.size() - step);
         }
     }
-    return (int)std::min(most, (size_t)workers);
+    return (int)most;
 }
 
 // Sets the tile and the way of the iterations of every matrix.
@@ -336,8 +343,26 @@ void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
         return std::max(1.0, n);
     };
     struct Load {
-        double total = 0, chain = 0;  // us: of all tasks, one after the other; of the longest chain of products
-        double time(double w) const { return std::max(total / w, chain) + 0.3 * std::min(total / w, chain); }
+        struct Step {
+            double tiles, cost;  // of a product; us: of one of its tasks
+        };
+        struct Chain {
+            std::vector<Step> steps;
+            double handovers;  // us
+        };
+        double total = 0, tasks = 0;  // us: of all tasks, one after the other; how many can be in work at once
+        std::vector<Chain> chains;    // of each shape: the products of one matrix, one behind the other
+        // us, of w workers: of the tasks spread over them, and of the longest chain
+        double time(double w) const
+        {
+            double chain = 0;
+            for (const Chain &c : chains) {
+                double one = c.handovers;
+                for (const Step &s : c.steps) one += std::ceil(s.tiles / w) * s.cost;
+                chain = std::max(chain, one);
+            }
+            return std::max(total / w, chain) + 0.3 * std::min(total / w, chain);
+        }
     };
     auto load = [&](bool precise, int tile, bool twos) {
         // us: of a step of K, of a task beside its steps, from a product's last step to the next one's first
@@ -345,24 +370,27 @@ void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
         Load l;
         const double square = all_tiles(tile, precise);
         const MuonMat *last = nullptr;
-        double last_total = 0;
+        double last_total = 0, last_tasks = 0;
         for (const MuonMat &m : *all) {
             if ((m.precise != 0) != precise) continue;
             if (!last || last->m != m.m || last->n != m.n) {
                 MuonMat probe = m;
                 set(probe, tile, twos, square);
-                double one = 0;
-                last_total = 0;
+                Load::Chain chain{{}, 0};
+                last_total = last_tasks = 0;
                 for (const MuonProduct &t : products_of(probe, c->cfg.steps)) {
                     const double rows = ceil_div(t.m, tile), cols = ceil_div(t.width, tile);
-                    const double tiles = (t.phase < MUON_UPDATE ? rows * (rows + 1) / 2 : rows * cols) * t.splits;
-                    last_total += tiles * (t.steps * step + task);
-                    one += std::ceil(tiles / workers) * (t.steps * step + task) + handover + (t.splits > 1 ? 2 : 0);
+                    const Load::Step s{(t.phase < MUON_UPDATE ? rows * (rows + 1) / 2 : rows * cols) * t.splits, t.steps * step + task};
+                    chain.steps.push_back(s);
+                    chain.handovers += handover + (t.splits > 1 ? 2 : 0);
+                    last_total += s.tiles * s.cost;
+                    last_tasks = std::max(last_tasks, s.tiles);
                 }
-                l.chain = std::max(l.chain, one);
+                l.chains.push_back(std::move(chain));
                 last = &m;
             }
             l.total += last_total;
+            l.tasks += last_tasks;
         }
         return l;
     };
@@ -371,17 +399,25 @@ void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
     bool best_twos = false;
     for (const int tile : {256, 128})
         for (const bool twos : {true, false}) {
-            const Load l = load(false, tile, twos);
-            if (!best_tile || l.time(workers) < best.time(workers)) best = l, best_tile = tile, best_twos = twos;
+            Load l = load(false, tile, twos);
+            if (!best_tile || l.time(workers) < best.time(workers)) best = std::move(l), best_tile = tile, best_twos = twos;
         }
     const Load side = load(true, 128, false);
     if (side.total > 0 && best.total > 0) {
-        // Both kinds at once: as few workers for the small ones as let them end well before the larger ones.  (Those of the larger ones stay until
-        // their last task is done: were they as many as the device holds, the small ones would come after them.)
-        auto both = [&](double w) { return std::max(1.5 * (side.total / w + side.chain), best.time(workers - w)); };
-        c->side_workers = 1;
-        for (int w = 2; w < (int)workers; ++w)
-            if (both(w) < both(c->side_workers)) c->side_workers = w;
+        // Both kinds at once, the workers divided between them so that the later of the two ends earliest, and the other early, too, where that costs
+        // little: never more for the small ones than they have tasks at once.  (Those of the larger ones stay until their last task is done: were they
+        // as many as the device holds, the small ones would come after them.)  Measured, us, larger / small ones alone, both, and the best of fourteen
+        // divisions from 1 to 70 workers: 512 x 512 / 64 x 64 93 / 78, 99, 98; 768 x 512 / 256 x 640 and 128 x 128 95 / 105, 117, 115; four of 1024 x
+        // 1024 / 256 x 512 195 / 101, 205, 207; 1024 x 1024 / thirty of 256 x 1024 117 / 287, 379, 348; eight of 512 x 512 / forty of 128 x 128 115 / 95, 181, 136.
+        auto both = [&](double w) {
+            const double small = side.time(w), large = best.time(workers - w);
+            return std::max(small, large) + 0.1 * std::min(small, large);
+        };
+        double least = 0;
+        for (int w = 1; w < (int)workers && (w == 1 || w <= side.tasks); w += 1 + w / 8) {
+            const double t = both(w);
+            if (w == 1 || t < least) least = t, c->side_workers = w;
+        }
     }
     const double squares[2] = {all_tiles(best_tile, false), all_tiles(best_tile, true)};
     for (MuonMat &m : *all) set(m, best_tile, best_twos, squares[m.precise != 0]);
@@ -470,7 +506,8 @@ demo_status make_tasks(demo_muon_ctx *c, Plan *plan)
 {
     for (Group &g : c->groups) {
         g.tasks = (long long)plan->tasks.size();
-        g.workers = add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.tile, plan);
+        g.at_once = add_tasks(c, plan->mats.data() + g.first_mat, g.first_mat, g.n_mats, g.tile, plan);
+        g.workers = std::min(g.at_once, workers_for(c, g.precise));
         g.n_tasks = (int)((long long)plan->tasks.size() - g.tasks);
         const auto waits = [&](long long k) { const MuonProduct &p = plan->products[(size_t)plan->tasks[(size_t)(g.tasks + k)].product]; return p.mat == g.first_mat && p.phase == MUON_POLY; };
         while (!waits(g.waiting)) ++g.waiting;  // (every matrix has that product)
@@ -622,6 +659,28 @@ bool usable(const void *const *p, int n)
 }  // namespace
 
 extern "C" {
+
+int demo_muon_plan(const demo_muon_config *cfg, const demo_tensor_desc *tensors, int n_tensors, int sm_count, int *groups, int most_groups)
+{
+    try {
+        demo_muon_ctx c;
+        c.cfg = *cfg;
+        c.n_tensors = n_tensors;
+        c.launch.sm_count = sm_count;
+        c.descs.assign(tensors, tensors + n_tensors);
+        Plan plan;
+        if (make_plan(&c, &plan) != DEMO_OK || make_tasks(&c, &plan) != DEMO_OK) return -1;
+        int n = 0;
+        for (const Group &g : c.groups)
+            if (n < most_groups) {
+                int *to = groups + 6 * n++;
+                to[0] = g.precise, to[1] = g.tile, to[2] = g.n_mats, to[3] = g.n_tasks, to[4] = g.at_once, to[5] = g.workers;
+            }
+        return (int)c.groups.size();
+    } catch (const std::exception &) {
+        return -1;
+    }
+}
 
 demo_status demo_muon_init(demo_muon_ctx **out, const demo_muon_config *cfg, const demo_tensor_desc *tensors, int32_t n_tensors, int32_t cuda_device)
 {
