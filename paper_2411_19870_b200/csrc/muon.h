@@ -143,6 +143,6 @@ cudaError_t muon_launch_products(int tile, bool precise, const MuonArgs &a, cons
 constexpr int muon_k_step(int tile) { return 16384 / tile; }
 constexpr int muon_epilogue_warps(int tile) { return tile == 256 ? 16 : 8; }
 
-// How a set would be worked on by a device of `sm_count` SMs; needs none (for tests).  Of each group six numbers: 1 where products take the lo parts, the
-// tiles' side, matrices, tasks, tasks that can be in work at once, workers.  Returns how many groups there are, -1 on failure.
+// How a set would be worked on by a device of `sm_count` SMs; needs none (for tests).  Of each group seven numbers: 1 where products take the lo parts, the
+// tiles' side, matrices, tasks, tasks that can be in work at once, workers, 1 where its first matrix does the first two iterations in one.  Returns how many groups there are, -1 on failure.
 extern "C" int demo_muon_plan(const demo_muon_config *cfg, const demo_tensor_desc *tensors, int n_tensors, int sm_count, int *groups, int most_groups);

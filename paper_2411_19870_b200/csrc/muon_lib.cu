@@ -673,8 +673,9 @@ int demo_muon_plan(const demo_muon_config *cfg, const demo_tensor_desc *tensors,
         int n = 0;
         for (const Group &g : c.groups)
             if (n < most_groups) {
-                int *to = groups + 6 * n++;
+                int *to = groups + 7 * n++;
                 to[0] = g.precise, to[1] = g.tile, to[2] = g.n_mats, to[3] = g.n_tasks, to[4] = g.at_once, to[5] = g.workers;
+                to[6] = plan.mats[(size_t)g.first_mat].twos;
             }
         return (int)c.groups.size();
     } catch (const std::exception &) {

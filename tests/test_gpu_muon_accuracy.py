@@ -69,3 +69,29 @@ def test_long_sums(shape, count, kind):
         assert error(shape, count, kind) <= 2e-5 + 6e-5  # (one row: of full rank)
     else:
         assert error(shape, count, kind) <= documented(shape, kind)
+
+
+# around the limit of the 22-bit products, and well on either side
+SIZES = [((64, 64), 1), ((128, 300), 1), ((257, 257), 1), ((300, 700), 1), ((700, 301), 1), ((384, 384), 1), ((384, 1537), 1), ((1000, 383), 40),
+         ((385, 385), 1), ((385, 386), 160), ((390, 1533), 1), ((390, 1533), 120), ((1201, 400), 1), ((512, 2048), 40), ((1024, 1024), 1)]
+
+
+@pytest.mark.parametrize("shape,count", SIZES)
+@pytest.mark.parametrize("kind", ["gaussian", "rows", "positive", "signs"])
+def test_full_rank(shape, count, kind):
+    if kind == "signs":  # (signs of Gaussian values: roundings of one size, but the entries' sums average them out)
+        assert error(shape, count, kind) <= documented(shape, "gaussian")
+    else:
+        assert error(shape, count, kind) <= documented(shape, kind)
+
+
+@pytest.mark.parametrize("shape,count", SIZES)
+@pytest.mark.parametrize("kind", ["1", "2", "5", "32", "128"])
+def test_low_rank(shape, count, kind):
+    assert error(shape, count, kind) <= documented(shape, kind)
+
+
+@pytest.mark.parametrize("shape,count", SIZES)
+@pytest.mark.parametrize("kind", ["equal", "equal rows", "equal columns", "blocks"])
+def test_equal_entries(shape, count, kind):
+    assert error(shape, count, kind) <= documented(shape, kind)

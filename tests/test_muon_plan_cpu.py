@@ -1,25 +1,9 @@
 """How the workers of a device of 148 SMs are divided among the matrices of a set: the plan, made without a device."""
-import ctypes
-
 import pytest
 
-from paper_2411_19870_b200 import binding
+from tests.muon_plan import plan
 
 WORKERS = 148 // 2
-
-
-def plan(shapes):
-    """Of each group: 22 bits or 11, tile, matrices, tasks, tasks at once, workers."""
-    lib = binding.load_library()
-    cfg = binding.DemoMuonConfig(0.95, 1, 5, (ctypes.c_float * 3)(3.4445, -4.7750, 2.0315), 1e-7, 1e-3, 0.1, 2, binding.DEMO_BF16)
-    descs = (binding.DemoTensorDesc * len(shapes))()
-    for d, s in zip(descs, shapes):
-        d.ndim, d.shape[0], d.shape[1] = 2, s[0], s[1]
-    most = 64
-    out = (ctypes.c_int * (6 * most))()
-    n = lib.demo_muon_plan(ctypes.byref(cfg), descs, len(shapes), 148, out, most)
-    assert 0 < n <= most
-    return [tuple(out[6 * i:6 * i + 6]) for i in range(n)]
 
 
 MIXED = [[(512, 512), (64, 64)], [(1024, 1024), (10, 20)], [(700, 500), (500, 1400), (256, 300)], [(768, 512), (256, 640), (128, 128)],
