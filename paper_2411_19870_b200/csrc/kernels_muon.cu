@@ -16,8 +16,8 @@
 //     through fp16: with P = D + E, Q = D' + E', P Q = D D' + D E' + E D' + E E', and only E E' is a product on the tensor cores; and that
 //     of X X^T is the one of X's fp32 values (muon.h, MUON_REST).
 // Relative error of the result against 64 bits, 1024 x 4096: Gaussian 3e-4, of rank 1, 32 and 128 9e-4, 6e-4 and 9e-4; 400 x 1200 5e-4 and 1.4e-3,
-// 1.2e-3, 1.7e-3 (plain bf16 operands, 1024 x 4096: Gaussian 1.3e-2, of rank 1 and 32 1.2 and 0.2; fp16: 1.7e-3, 0.15 and 0.03).  It grows as
-// matrices shrink, so those of up to 384 rows take the lo parts of the products' operands, too.  More iterations in one would multiply less (all
+// 1.2e-3, 1.7e-3 (plain bf16 operands, 1024 x 4096: Gaussian 1.3e-2, of rank 1 and 32 1.2 and 0.2; fp16: 1.7e-3, 0.15 and 0.03).  Equal entries are
+// rounded alike, which nothing averages out: all entries equal, 512 x 512 1.1e-2, 1111 x 3001 2.2e-2.  The error grows as matrices shrink, so those of up to 384 rows take the lo parts of the products' operands, too.  More iterations in one would multiply less (all
 // five 29 m^3 for n = 4 m instead of 56), but their B' B is rounded to 11 bits after the last one that could take noise away: [1, 2, 2] has up to
 // five times the error where the rank is low, [5] an error of 0.15.
 #include <cuda_bf16.h>
@@ -714,8 +714,8 @@ struct alignas(16) RingEntry {
 
 // All products of all iterations, by persistent workers, pairs of CTAs.  Tasks are drawn in the list's order from one counter, so
 // whatever a task waits for is done already or in the hands of a worker that runs: no worker has to be resident for another to go on.
-// Two warps load, one each operand, one issues the MMAs, eight read accumulators back: two of them, so that the products of a task run beside the epilogue
-// of the one before.  A fourth kind of warp schedules: that of a worker's first CTA draws the tasks and waits until they may start, and in
+// Two warps load, one each operand, one issues the MMAs, sixteen (eight in tiles of 128) read accumulators back.  There are two accumulators, so that the
+// products of a task run beside the epilogue of the one before.  A fourth kind of warp schedules: that of a worker's first CTA draws the tasks and waits until they may start, and in
 // both CTAs it puts what the others need to know of one into a ring, up to four ahead (by the loading warp itself: its look-ups and waits,
 // 3500 cycles a task, leave the tensor core without data).
 // Symmetric matrices exist above the diagonal only: left of it a panel's operand is loaded from the rows above, as its transpose.
@@ -1049,6 +1049,7 @@ __global__ void __launch_bounds__(Shape<TILE>::THREADS, 1) muon_products_kernel(
                     if (before == (unsigned)t.splits - 1u) atomicExch(count, 0u);  // for the next iteration
                 }
                 mine = __shfl_sync(0xffffffffu, before, 0) == (unsigned)t.splits - 1u;
+                __syncwarp();  // (what the first lane's fence lets it see, the others see, too: a shuffle alone orders no memory)
                 if (!mine) blocks = 0;
             }
             auto each_block = [&](auto use) {

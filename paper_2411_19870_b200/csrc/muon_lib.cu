@@ -36,8 +36,9 @@ enum { FROM_ORTHOGONALIZE = 0, FROM_STEP = 1, FROM_DECODE = 2, ENTRY_POINTS = 3 
 constexpr long long GROUP_ELEMENTS = 128LL << 20;  // workspace: 8 bytes for each, and up to 18 bytes for each of the square matrices beside X
 constexpr size_t GROUP_BYTES = 26 * (size_t)GROUP_ELEMENTS;  // of their workspace: thin matrices take more than 26 bytes an element, up to 145 where there is one row
 // Up to here the products take the lo parts, too (kernels_muon.cu): what 11 bits lose grows as matrices shrink, and small products are quick.
-// (384: an error of 1.6e-3 where the rank is low, as 384 x 768 decoded from few records, is 1e-5, for 113 us instead of 93, fourteen of 384 x 384 135
-// instead of 113, sixty of 384 x 1536 1360 instead of 800.  512: five of 512 x 4608 would take twice as long.)
+// (At 384 rows an error of 1.4e-3 where the rank is 128 becomes 1e-5, for 111 us instead of 93 of 384 x 768, 134 instead of 111 of fourteen of 384 x 384, 1324
+// instead of 838 of sixty of 384 x 1536.  At 512 rows 1.3e-3 is left, and one matrix would take 113 us instead of 93, 24 of 512 x 512 351 instead of 260,
+// 24 of 512 x 2048 1013 instead of 541.)
 constexpr int PRECISE_SIDE = 384;
 constexpr long long WAIT_CYCLES = 20000000000LL;  // ~10 s: what is waited for may be other workers' tasks, long ones for large matrices
 
@@ -67,7 +68,7 @@ struct demo_muon_ctx {
     int side_workers = 0;   // workers of the precise matrices where there are others, too
     int *d_status = nullptr;
     // Where there are matrices of both kinds, the precise ones go through the iterations beside the others, on a stream of the context's own,
-    // which the caller's stream waits for (five matrices of 512 rows and one of 147: 344 us, the five alone 335, the one 107).
+    // which the caller's stream waits for (five matrices of 512 rows and one of 147: 350 us, the five alone 341, the one 106).
     cudaStream_t side_stream = nullptr;
     cudaEvent_t fork = nullptr, join = nullptr;
     PointerTable tables[ENTRY_POINTS];  // inputs, outputs, and momenta where they are the caller's
@@ -324,10 +325,10 @@ void choose_shapes(demo_muon_ctx *c, std::vector<MuonMat> *all)
         // Sums of up to 2048 elements (8192 where the products are of 11 bits) at a time for their exactness: what the tensor core cuts off all goes
         // one way (160 of 64 x 8192, Gaussian / all entries equal: error 4.9e-5 / 5.2e-4 in 3.59 ms at 8192 at a time, 1.1e-5 / 6.4e-5 in 3.66 ms at
         // 2048; 50304 x 384 692, 722, 808 us at 8192, 4096, 2048; 60 of 400 x 32768, all equal: 1.5e-2 in 16.3 ms at 32768, 3e-3 in 14.2 ms at 8192).
-        // (From m = 8192 on parts of m, at most 32768: the other products' sums are as long, and a part takes 2 m^2 bytes.)  And long ones in three parts of
-        // 1024 or more where half of the workers have no tile.  Not more parts than workers: their way through memory costs more than they save.
-        // (Both with every second pair of iterations in one: 768 x 8000 207 us instead of 224, 2048 x 8192 594 instead of 618; 1024 x 4096 in 144
-        // parts instead of 72 206 instead of 189.)
+        // (From m = 8192 on parts of m, at most 32768: the other products' sums are as long, and a part takes 2 m^2 bytes.)
+        // And long ones in three parts of 1024 or more where half of the workers have no tile.  Not more parts than workers: their way through memory
+        // costs more than they save.  (In parts for the workers' sake / not / in twice as many: 768 x 8000 234 / 254 / 259 us, 2048 x 8192 654 / 772 / 748,
+        // 512 x 16000 260 / 286 / 300, 256 x 8000 165 / 171 / 165.)
         const int steps = ceil_div(m.n, muon_k_step(m.tile)), exact = ceil_div(m.n, m.precise ? 2048 : std::min(32768, std::max(8192, m.m)));
         const int parts = m.n / 1024, spread = parts > 2 && 2 * tiles <= workers ? std::min(parts, (int)(workers / tiles)) : 1;
         m.split_steps = ceil_div(steps, std::max(exact, spread));
